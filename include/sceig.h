@@ -14,7 +14,8 @@
  *     never frees or keeps them.  Inputs are const and never modified.  "host" pointers are ordinary
  *     host memory.
  *   - `stream` is a hipStream_t passed as void* (NULL = the default stream).  All device work is
- *     enqueued on it; every call returns after that work has completed (stream synchronised).
+ *     enqueued on it; every call returns after that work has completed (stream synchronised), except for
+ *     the calls that say that they only enqueue.
  *   - Return value: 0 = SC_OK; > 0 = soft condition, outputs are valid as described; < 0 = error,
  *     outputs are unspecified.  No C++ exception crosses this boundary.
  *   - CSR: rowptr int64[n+1] with rowptr[0] = 0, non-decreasing, rowptr[n] = nnz; col int32[nnz] in
@@ -485,6 +486,127 @@ int sc_knn_union_pairs(const int32_t* idx, const double* dist, int64_t n, int32_
 int sc_coo_to_csr(const int32_t* row, const int32_t* col, const double* val, int64_t nnz_in, int64_t n,
                   int32_t symmetrize, int64_t* rowptr_out, int32_t* col_out, double* val_out, int64_t* nnz_out,
                   void* stream);
+
+/* ----------------------------------------------------------------------------------------------------------------
+ * Cluster experts: a model per cluster, fed by a soft assignment of every row to a few clusters.  sc_route assigns (scores
+ * of n rows against k clusters, t clusters a row) and groups the n * t slots by cluster; sc_grouped_product multiplies every
+ * group with its cluster's matrix; sc_group_combine brings a row's t results together again.  sc_route_backward,
+ * sc_grouped_product (transposed), sc_grouped_gradient and sc_group_combine_backward are their gradients;
+ * sc_quantize_blocks and sc_grouped_product_e4m3 do the product with both factors in 8 bits.
+ *
+ * These calls only enqueue work on `stream`, allocate nothing and may be captured into a graph; everything they read or
+ * write must stay as it is until that work is done.  What they sum is held in fp32 and rounded once, to nearest even, where it
+ * is written; no result depends on the order in which workgroups run.  Element types (`dtype`): */
+#define SC_F32 0
+#define SC_BF16 1
+#define SC_F16 2
+/*
+ * Slots and groups: slot f = i * t + s is the s-th choice of row i.  offsets int32[groups + 1] (ascending, offsets[0] = 0): the
+ * grouped rows of group g are offsets[g] ... offsets[g + 1] - 1.  order int32: order[p] = the slot at grouped row p, -1 behind
+ * the last group.  place int32[n * t]: place[f] = the grouped row of slot f, -1 = none.  What offsets, order or place hold outside
+ * their ranges leads to no access outside the buffers: ranges are cut down to [0, rows), a source row that does not exist
+ * counts as zeros, a place that does not exist as none.
+ */
+
+/*
+ * The t clusters of largest score for every row, largest first, ties to the lowest index, and their softmax weights.
+ *   scores       device, n x k of dtype, row stride ld >= k
+ *   allowed      device bytes, n x k, row stride ld_allowed, or NULL: a zero rules the pair out whatever its score is; ld_allowed =
+ *                0: one row of k bytes for all rows.  A score of -infinity or NaN is ruled out too; a row whose largest score
+ *                is +infinity gets NaN weights
+ *   normalize    nonzero: softmax over the chosen clusters; 0: over all that are not ruled out
+ *   idx_out      device int32[n * t]: -1 where fewer than t clusters were left
+ *   weight_out   device fp32[n * t]: 0 there
+ *   offsets_out, order_out, place_out  device int32[k + 1], int32[n * t], int32[n * t]: the slots with a cluster, sorted
+ *                by cluster, in slot order within a cluster
+ *   work         device, at least sc_route_workspace_bytes
+ * 1 <= k <= 4096, 1 <= t <= min(k, 16), n * t <= 2^31 - 1, else SC_EDOMAIN.
+ */
+int sc_route_workspace_bytes(int64_t n, int32_t k, int32_t t, size_t* bytes_out);
+int sc_route(const void* scores, int32_t dtype, int64_t ld, const uint8_t* allowed, int64_t ld_allowed, int64_t n, int32_t k,
+             int32_t t, int32_t normalize, int32_t* idx_out, float* weight_out, int32_t* offsets_out, int32_t* order_out,
+             int32_t* place_out, void* work, size_t work_bytes, void* stream);
+
+/*
+ * Gradient of the scores from that of the weights: with p the softmax over the chosen (normalize) or all clusters that are not
+ * ruled out and c = sum_s weight_s dweight_s, dscores_j = p_j (dweight of the slot that chose j, or 0, - c); 0 where p is.
+ *   scores, allowed, ..., normalize  as sc_route got them (scores and allowed are read for normalize = 0 only)
+ *   idx, weight  as sc_route wrote them;  dweight  device fp32[n * t], not read where idx is -1
+ *   dscores_out  device, n x k of dtype, row stride ldd >= k
+ */
+int sc_route_backward(const void* scores, int32_t dtype, int64_t ld, const uint8_t* allowed, int64_t ld_allowed, int64_t n,
+                      int32_t k, int32_t t, int32_t normalize, const int32_t* idx, const float* weight, const float* dweight,
+                      void* dscores_out, int64_t ldd, void* stream);
+
+/*
+ * y_p = W_g x_p (transpose = 0) or W_g^T x_p for every row p of every group g; rows of y behind the last group are zero.
+ *   x        device, n_x rows of K (transpose: N) elements, row stride ldx; x_p is row order[p] / slots of x, or row p where
+ *            order is NULL (slots is then not read)
+ *   w        device, groups x N x K: element (g, o, c) at w[g * ldg + o * ldw + c], ldw >= K, ldg >= 0
+ *   offsets, order  as above
+ *   y        device, rows x N (transpose: K), row stride ldy; may not overlap an input
+ * x, w and y are of dtype.  Rows of any length, stride and alignment; whole 16-byte pieces are quickest.
+ */
+int sc_grouped_product(const void* x, int64_t ldx, int64_t n_x, const void* w, int64_t ldw, int64_t ldg, int32_t dtype,
+                       const int32_t* offsets, const int32_t* order, int32_t slots, int64_t rows, int32_t groups, int32_t N,
+                       int32_t K, int32_t transpose, void* y, int64_t ldy, void* stream);
+
+/*
+ * Gradient of the matrices: dw_g = sum over the rows p of group g of dy_p x_p^T; zero for a group without rows.
+ *   dy       device, rows x N, row stride lddy;   x, order, slots  as for sc_grouped_product (rows of K elements)
+ *   dw_out   device, groups x N x K of dtype, strides ldw >= K and ldg >= N * ldw
+ *   work     device, at least sc_grouped_gradient_workspace_bytes (which may be 0: then NULL will do)
+ */
+int sc_grouped_gradient_workspace_bytes(int64_t rows, int32_t groups, int32_t N, int32_t K, int32_t dtype, size_t* bytes_out);
+int sc_grouped_gradient(const void* dy, int64_t lddy, const void* x, int64_t ldx, int64_t n_x, int32_t dtype,
+                        const int32_t* offsets, const int32_t* order, int32_t slots, int64_t rows, int32_t groups, int32_t N,
+                        int32_t K, void* dw_out, int64_t ldw, int64_t ldg, void* work, size_t work_bytes, void* stream);
+
+/*
+ * out_i = sum over s of weight(i, s) z_place(i,s), slots without a place left out; a row without any gets zeros.
+ *   z        device, rows x d of dtype, row stride ldz;  place, weight  device, n x t; weight NULL: all ones
+ *   out      device, n x d of dtype, row stride ldo
+ * With weight NULL this is also the gradient of x in sc_grouped_product with an order: the grouped gradients of a row's
+ * slots, added up.
+ */
+int sc_group_combine(const void* z, int32_t dtype, int64_t ldz, int64_t rows, const int32_t* place, const float* weight,
+                     int64_t n, int32_t t, int32_t d, void* out, int64_t ldo, void* stream);
+
+/*
+ * dz_place(i,s) = weight(i, s) dout_i, rows p of dz with order[p] < 0 zero, and dweight(i, s) = <dout_i, z_place(i,s)> (0
+ * without a place).
+ *   dweight_out  device fp32[n * t], or NULL: not wanted, z is then not read and may be NULL
+ */
+int sc_group_combine_backward(const void* dout, int32_t dtype, int64_t ldo, const void* z, int64_t ldz, int64_t rows,
+                              const int32_t* place, const float* weight, const int32_t* order, int64_t n, int32_t t, int32_t d,
+                              void* dz_out, int64_t lddz, float* dweight_out, void* stream);
+
+/*
+ * 8-bit form of a matrix: every row in blocks of 128 (the last one filled up with zeros), a block as 128 numbers of 4 bits of
+ * exponent and 3 of fraction (bias 7, no infinities, largest 448) and one power of two 2^(byte - 127), byte 255 = NaN.
+ *   x        device, rows x K of dtype, row stride ldx
+ *   q_out    device bytes, row stride ldq >= K rounded up to a multiple of 128
+ *   scale_out device bytes, row stride ld_scale >= ceil(K / 128)
+ * sc_quantize_blocks takes the smallest power of two (at least 2^-127; 1 for zeros) that makes the block's largest finite
+ * magnitude fit, and rounds every value once, to nearest even; what is not finite becomes NaN.  sc_dequantize_blocks writes what
+ * they stand for, rounded to dtype (fp32 holds all of them below 2^128; from 2^-126 up so does bf16).
+ */
+int sc_quantize_blocks(const void* x, int32_t dtype, int64_t ldx, int64_t rows, int32_t K, uint8_t* q_out, int64_t ldq,
+                       uint8_t* scale_out, int64_t ld_scale, void* stream);
+int sc_dequantize_blocks(const uint8_t* q, int64_t ldq, const uint8_t* scale, int64_t ld_scale, int64_t rows, int32_t K,
+                         void* x_out, int32_t dtype, int64_t ldx, void* stream);
+
+/*
+ * sc_grouped_product (transpose = 0) with x and w in the 8-bit form; y of dtype.  Sums are in fp32, except that for a y of 16
+ * bits the matrix instructions add every eight neighbouring products with 14 bits below the largest of them first.
+ *   xq, xscale  n_x rows;  wq, wscale  element (g, o, c) at wq[g * ldg + o * ldw + c], its scale at
+ *               wscale[g * ldg_scale + o * ldw_scale + c / 128]
+ * xq and wq 16-byte aligned, their strides multiples of 16, rows filled up with zeros to whole blocks (else SC_EDOMAIN).
+ */
+int sc_grouped_product_e4m3(const uint8_t* xq, int64_t ldx, const uint8_t* xscale, int64_t ldx_scale, int64_t n_x,
+                            const uint8_t* wq, int64_t ldw, int64_t ldg, const uint8_t* wscale, int64_t ldw_scale,
+                            int64_t ldg_scale, const int32_t* offsets, const int32_t* order, int32_t slots, int64_t rows,
+                            int32_t groups, int32_t N, int32_t K, int32_t dtype, void* y, int64_t ldy, void* stream);
 
 const char* sc_strerror(int code);
 int sc_version(void);

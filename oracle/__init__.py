@@ -14,6 +14,7 @@ Contents
                 (the restarted Lanczos of Section IV-B / Algorithm 3, made multiplicity-safe).
 ``components``  exact spectrum by connected components: closed-form null space
                 D^1/2 1_C / sqrt(vol(C)) plus per-component eigenproblems.
+``experts``     cluster experts: assignment, products by group, weighted sum, 8-bit blocks, gradients.
 ``compare``     residuals, principal angles and containment defects used by the parity tests.
 
 Every function is pinned by ``tests/test_oracle_*.py`` to closed forms (ring, path, complete,

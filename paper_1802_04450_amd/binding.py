@@ -31,7 +31,10 @@ EXPORTS = ["sc_laplacian_eigsh", "sc_degree_scaling", "sc_spmm_normalized", "sc_
            "sc_chebyshev_filter", "sc_kmeanspp", "sc_kmeans_lloyd", "sc_kmeans", "sc_edge_similarity", "sc_knn_search", "sc_knn_union_pairs",
            "sc_coo_to_csr", "sc_workspace_bytes", "sc_scale_operator", "sc_laplacian_eigsh_ws",
            "sc_block_qr_noalloc", "sc_counter",
-           "sc_spmv_normalized_chain", "sc_probe_fp64_matrix_rate"]
+           "sc_spmv_normalized_chain", "sc_probe_fp64_matrix_rate",
+           "sc_route_workspace_bytes", "sc_route", "sc_route_backward", "sc_grouped_product",
+           "sc_grouped_gradient_workspace_bytes", "sc_grouped_gradient", "sc_group_combine", "sc_group_combine_backward",
+           "sc_quantize_blocks", "sc_dequantize_blocks", "sc_grouped_product_e4m3"]
 
 
 class ScOptions(ctypes.Structure):
@@ -114,6 +117,20 @@ def lib() -> ctypes.CDLL:
         _lib.sc_knn_union_pairs.argtypes = [vp, vp, i64, i32, dbl, vp, vp, vp, ctypes.POINTER(ctypes.c_int64), vp]
         _lib.sc_sym_eig.argtypes = [vp, i32, vp, vp]
         _lib.sc_sym_eig_top.argtypes = [vp, i32, i32, vp, vp]
+        size = ctypes.POINTER(ctypes.c_size_t)
+        _lib.sc_route_workspace_bytes.argtypes = [i64, i32, i32, size]
+        _lib.sc_route.argtypes = [vp, i32, i64, vp, i64, i64, i32, i32, i32, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
+        _lib.sc_route_backward.argtypes = [vp, i32, i64, vp, i64, i64, i32, i32, i32, vp, vp, vp, vp, i64, vp]
+        _lib.sc_grouped_product.argtypes = [vp, i64, i64, vp, i64, i64, i32, vp, vp, i32, i64, i32, i32, i32, i32, vp, i64, vp]
+        _lib.sc_grouped_gradient_workspace_bytes.argtypes = [i64, i32, i32, i32, i32, size]
+        _lib.sc_grouped_gradient.argtypes = [vp, i64, vp, i64, i64, i32, vp, vp, i32, i64, i32, i32, i32, vp, i64, i64, vp,
+                                             ctypes.c_size_t, vp]
+        _lib.sc_group_combine.argtypes = [vp, i32, i64, i64, vp, vp, i64, i32, i32, vp, i64, vp]
+        _lib.sc_group_combine_backward.argtypes = [vp, i32, i64, vp, i64, i64, vp, vp, vp, i64, i32, i32, vp, i64, vp, vp]
+        _lib.sc_quantize_blocks.argtypes = [vp, i32, i64, i64, i32, vp, i64, vp, i64, vp]
+        _lib.sc_dequantize_blocks.argtypes = [vp, i64, vp, i64, i64, i32, vp, i32, i64, vp]
+        _lib.sc_grouped_product_e4m3.argtypes = [vp, i64, vp, i64, i64, vp, i64, i64, vp, i64, i64, vp, vp, i32, i64, i32, i32,
+                                                 i32, i32, vp, i64, vp]
         for name in EXPORTS:
             getattr(_lib, name).restype = ctypes.c_int
         _lib.sc_strerror.restype = ctypes.c_char_p
@@ -492,6 +509,244 @@ def sc_knn_union_pairs(idx, dist, sigma: float = 0.0):
     _check(code)
     m = npairs.value
     return eu[:m], ev[:m], val[:m]
+
+
+# ---- cluster experts ---------------------------------------------------------------------------
+# These calls only enqueue work on the current stream; synchronise before reading results on the host.
+SC_F32, SC_BF16, SC_F16 = 0, 1, 2
+
+
+def _dtype(t) -> int:
+    import torch
+    kinds = {torch.float32: SC_F32, torch.bfloat16: SC_BF16, torch.float16: SC_F16}
+    assert t in kinds, t
+    return kinds[t]
+
+
+def _matrix(t, device=None):
+    """A device tensor of one of the three types whose rows are contiguous (strided rows are taken as they are)."""
+    _dtype(t.dtype)
+    assert t.is_cuda and (device is None or t.device == device), (t.device, device)
+    assert t.numel() == 0 or t.shape[-1] <= 1 or t.stride(-1) == 1, t.stride()
+    return t
+
+
+def _ld(t, dim: int = 0) -> int:
+    """Row stride of a matrix in elements (that of a single row does not matter)."""
+    least = t.shape[-1]
+    for d in range(dim + 1, t.dim() - 1):
+        least *= t.shape[d]
+    return t.stride(dim) if t.shape[dim] > 1 else max(least, 1)
+
+
+def _ints(t, count, device):
+    import torch
+    _dev(t, torch.int32)
+    assert t.device == device and (count is None or t.numel() == count), (t.device, t.shape, count)
+    return t
+
+
+def _allowed(allowed, n: int, k: int, device):
+    import torch
+    if allowed is None:
+        return None, 0
+    assert allowed.dtype in (torch.bool, torch.uint8) and allowed.device == device, (allowed.dtype, allowed.device)
+    assert tuple(allowed.shape) in ((k,), (n, k)), allowed.shape
+    assert allowed.shape[-1] <= 1 or allowed.stride(-1) == 1, allowed.stride()
+    return allowed, 0 if allowed.dim() == 1 else allowed.stride(0) if n > 1 else k
+
+
+def sc_route(scores, t: int, allowed=None, normalize: bool = True):
+    """The t best of k clusters for every row of scores ((n, k) device, fp32, bf16 or fp16).  allowed: bool (n, k) or (k,).
+    Returns (idx int32 (n, t), weight fp32 (n, t), offsets int32[k + 1], order int32[n * t], place int32 (n, t)) device."""
+    import torch
+    _matrix(scores)
+    n, k = scores.shape
+    dev = scores.device
+    allowed, lda = _allowed(allowed, n, k, dev)
+    slots = max(t, 0)
+    idx = torch.empty((n, slots), dtype=torch.int32, device=dev)
+    weight = torch.empty((n, slots), dtype=torch.float32, device=dev)
+    offsets = torch.empty(k + 1, dtype=torch.int32, device=dev)
+    order = torch.empty(n * slots, dtype=torch.int32, device=dev)
+    place = torch.empty((n, slots), dtype=torch.int32, device=dev)
+    need = ctypes.c_size_t(0)
+    _check(lib().sc_route_workspace_bytes(n, k, t, ctypes.byref(need)))
+    work = torch.empty(need.value, dtype=torch.uint8, device=dev)
+    with torch.cuda.device(dev):
+        code = lib().sc_route(_ptr(scores), _dtype(scores.dtype), _ld(scores), _ptr(allowed), lda, n, k, t, int(normalize),
+                              _ptr(idx), _ptr(weight), _ptr(offsets), _ptr(order), _ptr(place), _ptr(work), need.value,
+                              _stream())
+    _check(code)
+    return idx, weight, offsets, order, place
+
+
+def sc_route_backward(scores, idx, weight, dweight, allowed=None, normalize: bool = True):
+    """Gradient of the scores ((n, k), their type) from that of the weights (fp32 (n, t))."""
+    import torch
+    _matrix(scores)
+    n, k = scores.shape
+    t = idx.shape[1]
+    dev = scores.device
+    allowed, lda = _allowed(allowed, n, k, dev)
+    _ints(idx, n * t, dev), _dev(weight, torch.float32), _dev(dweight, torch.float32)
+    assert weight.shape == idx.shape == dweight.shape, (weight.shape, idx.shape, dweight.shape)
+    out = torch.empty((n, k), dtype=scores.dtype, device=dev)
+    with torch.cuda.device(dev):
+        code = lib().sc_route_backward(_ptr(scores), _dtype(scores.dtype), _ld(scores), _ptr(allowed), lda, n, k, t,
+                                       int(normalize), _ptr(idx), _ptr(weight), _ptr(dweight), _ptr(out), k, _stream())
+    _check(code)
+    return out
+
+
+def sc_grouped_product(x, w, offsets, order=None, slots: int = 1, transpose: bool = False, out=None):
+    """y_p = w[g] @ x[order[p] // slots] (transpose: w[g].T @ ...) for the rows p of every group g.  x (n_x, K) (transpose:
+    (n_x, N)), w (groups, N, K), offsets int32[groups + 1], order int32[rows] or None (row p of x itself).  Returns (rows, N)
+    (transpose: (rows, K)); rows behind the last group are zero."""
+    import torch
+    _matrix(x), _matrix(w, x.device)
+    assert x.dtype == w.dtype, (x.dtype, w.dtype)
+    groups, N, K = w.shape
+    dev = x.device
+    assert x.dim() == 2 and x.shape[1] == (N if transpose else K), (x.shape, w.shape)
+    _ints(offsets, groups + 1, dev)
+    rows = x.shape[0] if order is None else _ints(order, None, dev).numel()
+    cols = K if transpose else N
+    if out is None:
+        out = torch.empty((rows, cols), dtype=x.dtype, device=dev)
+    assert _matrix(out, dev).shape == (rows, cols) and out.dtype == x.dtype, (out.shape, out.dtype)
+    with torch.cuda.device(dev):
+        code = lib().sc_grouped_product(_ptr(x), _ld(x), x.shape[0], _ptr(w), _ld(w, 1), _ld(w), _dtype(x.dtype),
+                                        _ptr(offsets), _ptr(order), slots, rows, groups, N, K, int(transpose), _ptr(out),
+                                        _ld(out), _stream())
+    _check(code)
+    return out
+
+
+def sc_grouped_gradient(dy, x, offsets, order=None, slots: int = 1, out=None):
+    """dw[g] = sum over the rows p of group g of outer(dy[p], x[order[p] // slots]).  Returns (groups, N, K) of their type."""
+    import torch
+    _matrix(dy), _matrix(x, dy.device)
+    assert x.dtype == dy.dtype, (x.dtype, dy.dtype)
+    dev = dy.device
+    rows, N = dy.shape
+    K = x.shape[1]
+    groups = _ints(offsets, None, dev).numel() - 1
+    if order is None:
+        assert x.shape[0] == rows, (x.shape, dy.shape)
+    else:
+        _ints(order, rows, dev)
+    if out is None:
+        out = torch.empty((groups, N, K), dtype=dy.dtype, device=dev)
+    assert _matrix(out, dev).shape == (groups, N, K) and out.dtype == dy.dtype, (out.shape, out.dtype)
+    need = ctypes.c_size_t(0)
+    _check(lib().sc_grouped_gradient_workspace_bytes(rows, groups, N, K, _dtype(dy.dtype), ctypes.byref(need)))
+    work = torch.empty(need.value, dtype=torch.uint8, device=dev)
+    with torch.cuda.device(dev):
+        code = lib().sc_grouped_gradient(_ptr(dy), _ld(dy), _ptr(x), _ld(x), x.shape[0], _dtype(dy.dtype), _ptr(offsets),
+                                         _ptr(order), slots, rows, groups, N, K, _ptr(out), _ld(out, 1), _ld(out),
+                                         _ptr(work), need.value, _stream())
+    _check(code)
+    return out
+
+
+def sc_group_combine(z, place, weight=None):
+    """out[i] = sum over s of weight[i, s] z[place[i, s]], places < 0 left out.  z (rows, d), place int32 (n, t), weight fp32
+    (n, t) or None (ones).  Returns (n, d) of z's type."""
+    import torch
+    _matrix(z)
+    dev = z.device
+    n, t = place.shape
+    _ints(place, n * t, dev)
+    if weight is not None:
+        assert _dev(weight, torch.float32).shape == place.shape and weight.device == dev, (weight.shape, place.shape)
+    rows, d = z.shape
+    out = torch.empty((n, d), dtype=z.dtype, device=dev)
+    with torch.cuda.device(dev):
+        code = lib().sc_group_combine(_ptr(z), _dtype(z.dtype), _ld(z), rows, _ptr(place), _ptr(weight), n, t, d, _ptr(out),
+                                      max(d, 1), _stream())
+    _check(code)
+    return out
+
+
+def sc_group_combine_backward(dout, z, place, weight, order):
+    """Gradients of sc_group_combine: (dz (rows, d), dweight fp32 (n, t)); with weight None dweight is None."""
+    import torch
+    _matrix(dout), _matrix(z, dout.device)
+    dev = dout.device
+    n, t = place.shape
+    rows, d = z.shape
+    _ints(place, n * t, dev), _ints(order, rows, dev)
+    assert dout.shape == (n, d) and dout.dtype == z.dtype, (dout.shape, z.shape, dout.dtype, z.dtype)
+    dweight = None
+    if weight is not None:
+        assert _dev(weight, torch.float32).shape == place.shape and weight.device == dev, (weight.shape, place.shape)
+        dweight = torch.empty((n, t), dtype=torch.float32, device=dev)
+    dz = torch.empty((rows, d), dtype=z.dtype, device=dev)
+    with torch.cuda.device(dev):
+        code = lib().sc_group_combine_backward(_ptr(dout), _dtype(z.dtype), _ld(dout), _ptr(z), _ld(z), rows, _ptr(place),
+                                               _ptr(weight), _ptr(order), n, t, d, _ptr(dz), max(d, 1), _ptr(dweight),
+                                               _stream())
+    _check(code)
+    return dz, dweight
+
+
+def sc_quantize_blocks(x):
+    """8-bit form of x ((..., K) device): (q float8_e4m3fn (..., K rounded up to 128), scale uint8 (..., ceil(K / 128)), the
+    exponent of a block's power of two plus 127)."""
+    import torch
+    K = x.shape[-1]
+    x2 = _matrix(x if x.dim() == 2 else x.reshape(-1, K))
+    rows, blocks = x2.shape[0], -(-K // 128)
+    q = torch.empty((*x.shape[:-1], blocks * 128), dtype=torch.float8_e4m3fn, device=x.device)
+    scale = torch.empty((*x.shape[:-1], blocks), dtype=torch.uint8, device=x.device)
+    with torch.cuda.device(x.device):
+        code = lib().sc_quantize_blocks(_ptr(x2), _dtype(x.dtype), _ld(x2), rows, K, _ptr(q), blocks * 128, _ptr(scale),
+                                        blocks, _stream())
+    _check(code)
+    return q, scale
+
+
+def _blocks(q, scale, device=None):
+    import torch
+    _dev(q, torch.float8_e4m3fn), _dev(scale, torch.uint8)
+    assert q.device == scale.device and (device is None or q.device == device), (q.device, scale.device, device)
+    assert q.shape[-1] == 128 * scale.shape[-1] and q.shape[:-1] == scale.shape[:-1], (q.shape, scale.shape)
+
+
+def sc_dequantize_blocks(q, scale, K: Optional[int] = None, dtype=None):
+    """The first K values of every row that the 8-bit form stands for, (..., K) of dtype (default fp32)."""
+    import torch
+    _blocks(q, scale)
+    K = q.shape[-1] if K is None else K
+    assert q.shape[-1] - 128 < K <= q.shape[-1], (K, q.shape)
+    out = torch.empty((*q.shape[:-1], K), dtype=dtype or torch.float32, device=q.device)
+    with torch.cuda.device(q.device):
+        code = lib().sc_dequantize_blocks(_ptr(q), q.shape[-1], _ptr(scale), scale.shape[-1], out.numel() // K, K, _ptr(out),
+                                          _dtype(out.dtype), K, _stream())
+    _check(code)
+    return out
+
+
+def sc_grouped_product_e4m3(xq, xscale, wq, wscale, offsets, order=None, slots: int = 1, dtype=None, out=None):
+    """sc_grouped_product with both factors in the 8-bit form of sc_quantize_blocks: xq (n_x, Kp), wq (groups, N, Kp).  Returns
+    (rows, N) of dtype (default bf16)."""
+    import torch
+    _blocks(xq, xscale), _blocks(wq, wscale, xq.device)
+    groups, N, Kp = wq.shape
+    dev = xq.device
+    assert xq.dim() == 2 and xq.shape[1] == Kp, (xq.shape, wq.shape)
+    _ints(offsets, groups + 1, dev)
+    rows = xq.shape[0] if order is None else _ints(order, None, dev).numel()
+    if out is None:
+        out = torch.empty((rows, N), dtype=dtype or torch.bfloat16, device=dev)
+    assert _matrix(out, dev).shape == (rows, N), out.shape
+    with torch.cuda.device(dev):
+        code = lib().sc_grouped_product_e4m3(_ptr(xq), Kp, _ptr(xscale), Kp // 128, xq.shape[0], _ptr(wq), Kp, N * Kp,
+                                             _ptr(wscale), Kp // 128, N * (Kp // 128), _ptr(offsets), _ptr(order), slots,
+                                             rows, groups, N, Kp, _dtype(out.dtype), _ptr(out), _ld(out), _stream())
+    _check(code)
+    return out
 
 
 def sc_sym_eig(a: np.ndarray, vectors: bool = True) -> Tuple[np.ndarray, Optional[np.ndarray]]:

@@ -1,0 +1,84 @@
+// Launch wrappers of the operators of cluster experts: the assignment of rows to clusters (route.hip), the product of every
+// group of rows with its cluster's matrix in 16 and 32 bits (grouped.hip) and in 8 bits (e4m3.hip).  All pointers are device
+// pointers; every wrapper only enqueues work on `st` and returns hipGetLastError().  The sizes have been checked by the caller.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace sceig {
+
+enum { kF32 = 0, kBF16 = 1, kF16 = 2 };  // SC_F32, SC_BF16, SC_F16
+constexpr int kMaxRouteClusters = 4096;
+constexpr int kMaxRouteChoices = 16;
+constexpr int kScaleBlock = 128;  // values that share a scale in the 8-bit form
+
+inline size_t type_bytes(int dtype) { return dtype == kF32 ? 4 : 2; }
+
+// ---- route.hip ------------------------------------------------------------------------------------------------------
+size_t route_workspace(int64_t n, int k, int t);
+hipError_t launch_route(const void* scores, int dtype, int64_t ld, const uint8_t* allowed, int64_t lda, int64_t n, int k, int t,
+                        bool normalize, int32_t* idx, float* weight, int32_t* offsets, int32_t* order, int32_t* place,
+                        void* work, hipStream_t st);
+hipError_t launch_route_backward(const void* scores, int dtype, int64_t ld, const uint8_t* allowed, int64_t lda, int64_t n,
+                                 int k, int t, bool normalize, const int32_t* idx, const float* weight, const float* dweight,
+                                 void* dscores, int64_t ldd, hipStream_t st);
+hipError_t launch_group_combine(const void* z, int dtype, int64_t ldz, int64_t rows, const int32_t* place, const float* weight,
+                                int64_t n, int t, int d, void* out, int64_t ldo, hipStream_t st);
+hipError_t launch_group_combine_backward(const void* dout, int dtype, int64_t ldo, const void* z, int64_t ldz, int64_t rows,
+                                         const int32_t* place, const float* weight, const int32_t* order, int64_t n, int t,
+                                         int d, void* dz, int64_t lddz, float* dweight, hipStream_t st);
+
+// ---- grouped.hip ----------------------------------------------------------------------------------------------------
+// A product of groups of rows with a matrix per group.  Row p of group g is source row order[p] / slots of x (p without order).
+struct GroupedArgs {
+  const void* x;         // source rows, ldx
+  const void* w;         // groups x N x K: row o of group g at w + g * ldg + o * ldw
+  void* y;               // rows x (N or K), ldy
+  const int32_t* offsets;
+  const int32_t* order;  // may be null
+  int64_t ldx, ldw, ldg, ldy;
+  int64_t rows, xrows;   // rows of y; rows of x
+  int groups, slots;
+  int N, K;              // of w
+  int dtype;
+};
+hipError_t launch_grouped_product(const GroupedArgs& a, bool transpose, hipStream_t st);
+
+// dw_g = sum over the rows p of group g of dy_p x_p^T
+struct GradientArgs {
+  const void* dy;        // rows x N
+  const void* x;         // xrows x K
+  void* dw;              // groups x N x K
+  const int32_t* offsets;
+  const int32_t* order;
+  int64_t lddy, ldx, ldw, ldg;
+  int64_t rows, xrows;
+  int groups, slots;
+  int N, K;
+  int dtype;
+};
+hipError_t launch_grouped_gradient(const GradientArgs& a, hipStream_t st);
+
+// ---- e4m3.hip -------------------------------------------------------------------------------------------------------
+hipError_t launch_quantize_blocks(const void* x, int dtype, int64_t ldx, int64_t rows, int K, uint8_t* q, int64_t ldq,
+                                  uint8_t* scale, int64_t lds, hipStream_t st);
+hipError_t launch_dequantize_blocks(const uint8_t* q, int64_t ldq, const uint8_t* scale, int64_t lds, int64_t rows, int K,
+                                    void* x, int dtype, int64_t ldx, hipStream_t st);
+struct E4m3Args {
+  const uint8_t* x;      // xrows x Kp, Kp = K rounded up to whole blocks
+  const uint8_t* xs;     // xrows x Kp / 128
+  const uint8_t* w;      // groups x N x Kp
+  const uint8_t* ws;
+  void* y;
+  const int32_t* offsets;
+  const int32_t* order;
+  int64_t ldx, ldxs, ldw, ldws, ldg, ldgs, ldy;
+  int64_t rows, xrows;
+  int groups, slots;
+  int N, Kp;
+  int dtype;             // of y
+};
+hipError_t launch_grouped_product_e4m3(const E4m3Args& a, hipStream_t st);
+
+}  // namespace sceig

@@ -1,0 +1,147 @@
+// C entry points of the operators of cluster experts: checks of the arguments, then the launches.  Nothing here allocates or
+// throws.
+#include "../../include/sceig.h"
+#include "experts.h"
+
+#include <cmath>
+
+using namespace sceig;
+
+namespace {
+
+constexpr int64_t kMaxIndex = 0x7fffffff;
+
+bool known_type(int32_t dtype) { return dtype == SC_F32 || dtype == SC_BF16 || dtype == SC_F16; }
+int status(hipError_t e) {
+  if (e == hipSuccess) return SC_OK;
+  return e == hipErrorInvalidConfiguration ? SC_EDOMAIN : SC_EHIP;
+}
+hipStream_t as_stream(void* s) { return reinterpret_cast<hipStream_t>(s); }
+bool route_sizes(int64_t n, int32_t k, int32_t t) {
+  return n >= 0 && k >= 1 && k <= kMaxRouteClusters && t >= 1 && t <= k && t <= kMaxRouteChoices && n <= kMaxIndex / t;
+}
+// groups of rows: rows and slots as sc_route makes them
+bool group_sizes(int64_t rows, int64_t n_x, const int32_t* order, int32_t slots, int32_t groups, int32_t N, int32_t K) {
+  return rows >= 0 && rows <= kMaxIndex && n_x >= 0 && n_x <= kMaxIndex && groups >= 1 && groups <= (1 << 20) && N >= 1 && K >= 1 &&
+         (!order || slots >= 1);
+}
+
+}  // namespace
+
+extern "C" {
+
+int sc_route_workspace_bytes(int64_t n, int32_t k, int32_t t, size_t* bytes_out) {
+  if (!bytes_out) return SC_EINVAL;
+  if (n < 0) return SC_EINVAL;
+  if (!route_sizes(n, k, t)) return SC_EDOMAIN;
+  *bytes_out = route_workspace(n, k, t);
+  return SC_OK;
+}
+
+int sc_route(const void* scores, int32_t dtype, int64_t ld, const uint8_t* allowed, int64_t ld_allowed, int64_t n, int32_t k,
+             int32_t t, int32_t normalize, int32_t* idx_out, float* weight_out, int32_t* offsets_out, int32_t* order_out,
+             int32_t* place_out, void* work, size_t work_bytes, void* stream) {
+  if (n < 0 || !offsets_out || (n > 0 && (!scores || !idx_out || !weight_out || !order_out || !place_out))) return SC_EINVAL;
+  if (!known_type(dtype) || !route_sizes(n, k, t) || ld < k || (allowed && ld_allowed != 0 && ld_allowed < k)) return SC_EDOMAIN;
+  const size_t need = route_workspace(n, k, t);
+  if (need > 0 && !work) return SC_EINVAL;
+  if (work_bytes < need || reinterpret_cast<uintptr_t>(work) % 4 != 0) return SC_EDOMAIN;
+  return status(launch_route(scores, dtype, ld, allowed, ld_allowed, n, k, t, normalize != 0, idx_out, weight_out, offsets_out,
+                             order_out, place_out, work, as_stream(stream)));
+}
+
+int sc_route_backward(const void* scores, int32_t dtype, int64_t ld, const uint8_t* allowed, int64_t ld_allowed, int64_t n,
+                      int32_t k, int32_t t, int32_t normalize, const int32_t* idx, const float* weight, const float* dweight,
+                      void* dscores_out, int64_t ldd, void* stream) {
+  if (n < 0 || (n > 0 && ((!scores && !normalize) || !idx || !weight || !dweight || !dscores_out))) return SC_EINVAL;
+  if (!known_type(dtype) || !route_sizes(n, k, t) || (!normalize && ld < k) || ldd < k ||
+      (allowed && ld_allowed != 0 && ld_allowed < k))
+    return SC_EDOMAIN;
+  return status(launch_route_backward(scores, dtype, ld, allowed, ld_allowed, n, k, t, normalize != 0, idx, weight, dweight,
+                                      dscores_out, ldd, as_stream(stream)));
+}
+
+int sc_grouped_product(const void* x, int64_t ldx, int64_t n_x, const void* w, int64_t ldw, int64_t ldg, int32_t dtype,
+                       const int32_t* offsets, const int32_t* order, int32_t slots, int64_t rows, int32_t groups, int32_t N,
+                       int32_t K, int32_t transpose, void* y, int64_t ldy, void* stream) {
+  if (rows < 0 || n_x < 0 || !offsets || !w || (rows > 0 && (!x || !y))) return SC_EINVAL;
+  if (!known_type(dtype) || !group_sizes(rows, n_x, order, slots, groups, N, K) || ldx < (transpose ? N : K) || ldw < K || ldg < 0 ||
+      ldy < (transpose ? K : N))
+    return SC_EDOMAIN;
+  const GroupedArgs a{x, w, y, offsets, order, ldx, ldw, ldg, ldy, rows, n_x, groups, order ? slots : 1, N, K, dtype};
+  return status(launch_grouped_product(a, transpose != 0, as_stream(stream)));
+}
+
+int sc_grouped_gradient_workspace_bytes(int64_t rows, int32_t groups, int32_t N, int32_t K, int32_t dtype, size_t* bytes_out) {
+  if (!bytes_out || rows < 0) return SC_EINVAL;
+  if (!known_type(dtype) || !group_sizes(rows, rows, nullptr, 1, groups, N, K)) return SC_EDOMAIN;
+  *bytes_out = 0;
+  return SC_OK;
+}
+
+int sc_grouped_gradient(const void* dy, int64_t lddy, const void* x, int64_t ldx, int64_t n_x, int32_t dtype,
+                        const int32_t* offsets, const int32_t* order, int32_t slots, int64_t rows, int32_t groups, int32_t N,
+                        int32_t K, void* dw_out, int64_t ldw, int64_t ldg, void* work, size_t work_bytes, void* stream) {
+  (void)work;
+  (void)work_bytes;
+  if (rows < 0 || n_x < 0 || !offsets || !dw_out || (rows > 0 && (!dy || !x))) return SC_EINVAL;
+  if (!known_type(dtype) || !group_sizes(rows, n_x, order, slots, groups, N, K) || lddy < N || ldx < K || ldw < K ||
+      ldg < (int64_t)(N - 1) * ldw + K)
+    return SC_EDOMAIN;
+  const GradientArgs a{dy, x, dw_out, offsets, order, lddy, ldx, ldw, ldg, rows, n_x, groups, order ? slots : 1, N, K, dtype};
+  return status(launch_grouped_gradient(a, as_stream(stream)));
+}
+
+int sc_group_combine(const void* z, int32_t dtype, int64_t ldz, int64_t rows, const int32_t* place, const float* weight,
+                     int64_t n, int32_t t, int32_t d, void* out, int64_t ldo, void* stream) {
+  if (n < 0 || rows < 0 || (n > 0 && (!place || !out || (rows > 0 && !z)))) return SC_EINVAL;
+  if (!known_type(dtype) || rows > kMaxIndex || t < 1 || n > kMaxIndex / t || d < 1 || ldz < d || ldo < d) return SC_EDOMAIN;
+  return status(launch_group_combine(z, dtype, ldz, rows, place, weight, n, t, d, out, ldo, as_stream(stream)));
+}
+
+int sc_group_combine_backward(const void* dout, int32_t dtype, int64_t ldo, const void* z, int64_t ldz, int64_t rows,
+                              const int32_t* place, const float* weight, const int32_t* order, int64_t n, int32_t t, int32_t d,
+                              void* dz_out, int64_t lddz, float* dweight_out, void* stream) {
+  if (n < 0 || rows < 0 || (n > 0 && (!dout || !place)) || (rows > 0 && (!dz_out || !order)) ||
+      (dweight_out && rows > 0 && !z))
+    return SC_EINVAL;
+  if (!known_type(dtype) || rows > kMaxIndex || t < 1 || n > kMaxIndex / t || d < 1 || ldo < d || lddz < d ||
+      (dweight_out && ldz < d))
+    return SC_EDOMAIN;
+  return status(launch_group_combine_backward(dout, dtype, ldo, z, ldz, rows, place, weight, order, n, t, d, dz_out, lddz,
+                                              dweight_out, as_stream(stream)));
+}
+
+int sc_quantize_blocks(const void* x, int32_t dtype, int64_t ldx, int64_t rows, int32_t K, uint8_t* q_out, int64_t ldq,
+                       uint8_t* scale_out, int64_t ld_scale, void* stream) {
+  if (rows < 0 || (rows > 0 && (!x || !q_out || !scale_out))) return SC_EINVAL;
+  const int64_t blocks = ((int64_t)K + kScaleBlock - 1) / kScaleBlock;
+  if (!known_type(dtype) || K < 1 || K > (1 << 30) || ldx < K || ldq < blocks * kScaleBlock || ld_scale < blocks) return SC_EDOMAIN;
+  return status(launch_quantize_blocks(x, dtype, ldx, rows, K, q_out, ldq, scale_out, ld_scale, as_stream(stream)));
+}
+
+int sc_dequantize_blocks(const uint8_t* q, int64_t ldq, const uint8_t* scale, int64_t ld_scale, int64_t rows, int32_t K,
+                         void* x_out, int32_t dtype, int64_t ldx, void* stream) {
+  if (rows < 0 || (rows > 0 && (!q || !scale || !x_out))) return SC_EINVAL;
+  const int64_t blocks = ((int64_t)K + kScaleBlock - 1) / kScaleBlock;
+  if (!known_type(dtype) || K < 1 || K > (1 << 30) || ldx < K || ldq < blocks * kScaleBlock || ld_scale < blocks) return SC_EDOMAIN;
+  return status(launch_dequantize_blocks(q, ldq, scale, ld_scale, rows, K, x_out, dtype, ldx, as_stream(stream)));
+}
+
+int sc_grouped_product_e4m3(const uint8_t* xq, int64_t ldx, const uint8_t* xscale, int64_t ldx_scale, int64_t n_x,
+                            const uint8_t* wq, int64_t ldw, int64_t ldg, const uint8_t* wscale, int64_t ldw_scale,
+                            int64_t ldg_scale, const int32_t* offsets, const int32_t* order, int32_t slots, int64_t rows,
+                            int32_t groups, int32_t N, int32_t K, int32_t dtype, void* y, int64_t ldy, void* stream) {
+  if (rows < 0 || n_x < 0 || !offsets || !wq || !wscale || (rows > 0 && (!xq || !xscale || !y))) return SC_EINVAL;
+  if (K > (1 << 30) || !known_type(dtype) || !group_sizes(rows, n_x, order, slots, groups, N, K)) return SC_EDOMAIN;
+  const int64_t blocks = ((int64_t)K + kScaleBlock - 1) / kScaleBlock;
+  if (ldx < blocks * kScaleBlock || ldw < blocks * kScaleBlock || ldx_scale < blocks || ldw_scale < blocks || ldg < 0 ||
+      ldg_scale < 0 || ldy < N || ldx % 16 != 0 || ldw % 16 != 0 || ldg % 16 != 0 || reinterpret_cast<uintptr_t>(xq) % 16 != 0 ||
+      reinterpret_cast<uintptr_t>(wq) % 16 != 0)
+    return SC_EDOMAIN;
+  const E4m3Args a{xq, xscale, wq, wscale, y, offsets, order, ldx, ldx_scale, ldw, ldw_scale, ldg, ldg_scale, ldy,
+                   rows, n_x, groups, order ? slots : 1, N, (int)(blocks * kScaleBlock), dtype};
+  return status(launch_grouped_product_e4m3(a, as_stream(stream)));
+}
+
+}  // extern "C"

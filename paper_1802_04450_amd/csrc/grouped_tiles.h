@@ -1,0 +1,97 @@
+// Which part of a product by groups a workgroup computes (device code shared by the 16-, 32- and 8-bit kernels).
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace sceig {
+namespace {
+
+// Groups are [offsets[g], offsets[g + 1]), cut down to [0, rows) so that no offsets, whatever they hold, lead outside.  The
+// rows after the last group are one more group, `groups`, which is set to zero.
+struct GroupRange {
+  int64_t begin, end;
+};
+__device__ __forceinline__ GroupRange group_range(const int32_t* offsets, int groups, int64_t rows, int g) {
+  GroupRange r;
+  const int64_t b = offsets[g];
+  r.begin = b < 0 ? 0 : (b > rows ? rows : b);
+  const int64_t e = g < groups ? (int64_t)offsets[g + 1] : rows;
+  r.end = e < r.begin ? r.begin : (e > rows ? rows : e);
+  return r;
+}
+
+struct RowTile {
+  int group;      // -1: none
+  int64_t begin;  // first row of y
+  int count;      // rows of it that are the group's, at most BM
+  int col;        // column tile
+};
+
+// Every wave finds its tile by itself: a lane adds up the row tiles of consecutive groups, a scan over the lanes says which lane
+// holds the tile.  Consecutive workgroups go to the eight dies in turn, so a die gets a contiguous run of the tiles (all column
+// tiles of a row tile, then the next row tile of the same group): what its workgroups read at one time is shared in its L2.
+template <int BM>
+__device__ __forceinline__ RowTile find_tile(const int32_t* offsets, int groups, int64_t rows, int cols) {
+  const int lane = threadIdx.x & 63;
+  const int per = (groups + 1 + 63) / 64;
+  const int g0 = lane * per;
+  int mine = 0;
+  for (int u = 0; u < per; ++u) {
+    if (g0 + u > groups) break;
+    const GroupRange r = group_range(offsets, groups, rows, g0 + u);
+    mine += (int)((r.end - r.begin + BM - 1) / BM);
+  }
+  int sum = mine;
+#pragma unroll
+  for (int s = 1; s < 64; s <<= 1) {
+    const int o = __shfl_up(sum, s);
+    if (lane >= s) sum += o;
+  }
+  RowTile t;
+  t.group = -1;
+  t.begin = 0;
+  t.count = 0;
+  t.col = 0;
+  const int64_t total = (int64_t)__shfl(sum, 63) * cols;
+  const int64_t share = (total + 7) / 8;
+  const int64_t slot = blockIdx.x >> 3;
+  const int64_t at = (int64_t)(blockIdx.x & 7) * share + slot;
+  if (slot >= share || at >= total) return t;
+  const int row_tile = (int)(at / cols);
+  t.col = (int)(at - (int64_t)row_tile * cols);
+  const uint64_t has = __ballot(row_tile < sum);
+  const int owner = __ffsll((unsigned long long)has) - 1;
+  int left = row_tile - __shfl(sum - mine, owner);
+  const int first = owner * per;
+  for (int u = 0; u < per; ++u) {
+    if (first + u > groups) break;
+    const GroupRange r = group_range(offsets, groups, rows, first + u);
+    const int tiles = (int)((r.end - r.begin + BM - 1) / BM);
+    if (left < tiles) {
+      t.group = first + u;
+      t.begin = r.begin + (int64_t)left * BM;
+      const int64_t c = r.end - t.begin;
+      t.count = c < BM ? (int)c : BM;
+      break;
+    }
+    left -= tiles;
+  }
+  return t;
+}
+
+// Workgroups that find_tile needs at most: every group adds at most one tile that is not full, and no tile is without a row.
+inline int64_t tile_bound(int64_t rows, int groups, int bm, int64_t cols) {
+  const int64_t full = rows / bm + groups + 1;
+  const int64_t tiles = (full < rows ? full : rows) * cols;
+  return (tiles + 7) / 8 * 8;
+}
+
+// Source row of row p of a group, or -1: what `order` holds beyond [0, xrows * slots) reads as a row of zeros.
+__device__ __forceinline__ int64_t source_row(const int32_t* order, int64_t p, int slots, int64_t xrows) {
+  const int64_t r = order ? (order[p] < 0 ? -1 : (int64_t)((uint32_t)order[p] / (uint32_t)slots)) : p;
+  return r < xrows ? r : -1;
+}
+
+}  // namespace
+}  // namespace sceig

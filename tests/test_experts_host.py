@@ -1,0 +1,142 @@
+"""Cluster experts without a GPU: the oracle's pins (closed forms, gradients against differences) and the argument errors that the
+entry points decide before any GPU work."""
+import ctypes
+
+import numpy as np
+import pytest
+
+from oracle import experts as ox
+from paper_1802_04450_amd import binding
+
+
+def test_oracle_route_closed_forms():
+    s = np.array([[0.0, np.log(3.0), 0.0, -np.inf], [np.nan, 1.0, 1.0, 1.0], [-np.inf] * 4, [5.0, 5.0, 5.0, 5.0]])
+    idx, w, p = ox.route(s, 2)
+    assert idx.tolist() == [[1, 0], [1, 2], [-1, -1], [0, 1]]
+    np.testing.assert_allclose(w, [[0.75, 0.25], [0.5, 0.5], [0, 0], [0.5, 0.5]], atol=1e-15)
+    _, w, p = ox.route(s, 2, normalize=False)
+    np.testing.assert_allclose(w, [[0.6, 0.2], [1 / 3, 1 / 3], [0, 0], [0.25, 0.25]], atol=1e-15)
+    idx, w, _ = ox.route(s, 3, allowed=np.array([False, True, False, True]))
+    assert idx.tolist() == [[1, -1, -1], [1, 3, -1], [-1, -1, -1], [1, 3, -1]]
+    offsets, order, place = ox.grouping(idx, 4)
+    assert offsets.tolist() == [0, 0, 3, 3, 5] and order.tolist() == [0, 3, 9, 4, 10] + [-1] * 7
+    assert place.tolist() == [[0, -1, -1], [1, 3, -1], [-1, -1, -1], [2, 4, -1]]
+
+
+@pytest.mark.parametrize("normalize", [True, False])
+def test_oracle_route_gradient_against_differences(normalize):
+    rng = np.random.default_rng(1)
+    s, dw = rng.standard_normal((6, 7)), rng.standard_normal((6, 3))
+    idx, w, p = ox.route(s, 3, normalize=normalize)
+    ds = ox.route_backward(idx, w, p, dw)
+    for i in range(6):
+        for j in range(7):
+            a, b = s.copy(), s.copy()
+            a[i, j] += 1e-6
+            b[i, j] -= 1e-6
+            num = ((ox.route(a, 3, normalize=normalize)[1] - ox.route(b, 3, normalize=normalize)[1]) * dw).sum() / 2e-6
+            assert abs(num - ds[i, j]) < 1e-8
+
+
+def test_oracle_products_against_loops():
+    rng = np.random.default_rng(2)
+    idx = np.array([[0, 2], [2, -1], [1, 0]], dtype=np.int32)
+    offsets, order, place = ox.grouping(idx, 3)
+    x, w, weight = rng.standard_normal((3, 4)), rng.standard_normal((3, 5, 4)), rng.random((3, 2))
+    z, _ = ox.grouped_product(x, w, offsets, order, 2)
+    out, _ = ox.combine(z, place, weight)
+    for i in range(3):
+        ref = sum(weight[i, s] * w[idx[i, s]] @ x[i] for s in range(2) if idx[i, s] >= 0)
+        np.testing.assert_allclose(out[i], ref, atol=1e-14)
+    # linear in each factor: the loss <dout, out> is recovered from every gradient
+    dout = rng.standard_normal((3, 5))
+    dz, dweight, _ = ox.combine_backward(dout, z, place, weight)
+    loss = (dout * out).sum()
+    np.testing.assert_allclose((dweight * weight).sum(), loss, atol=1e-12)
+    dw, _ = ox.grouped_gradient(dz, x, offsets, order, 2)
+    np.testing.assert_allclose((dw * w).sum(), loss, atol=1e-12)
+    dx, _ = ox.combine(ox.grouped_product(dz, w, offsets, transpose=True)[0], place)
+    np.testing.assert_allclose((dx * x).sum(), loss, atol=1e-12)
+
+
+def test_oracle_blocks_closed_forms():
+    tab = ox.e4m3_values()
+    assert tab[-1] == 448.0 and tab[1] == 2.0 ** -9 and tab[8] == 2.0 ** -6 and np.all(np.diff(tab) > 0)
+    x = np.zeros((1, 130))
+    x[0, :127] = tab
+    x[0, 128:] = [900.0, -450.0]
+    code, e, val = ox.quantize_blocks(x)
+    assert e.tolist() == [[127, 129]] and np.array_equal(val[0, :127], tab) and np.array_equal(code[0, :127], np.arange(127))
+    assert val[0, 128:131].tolist() == [896.0, -448.0, 0.0]                # 225 -> 224, 112.5 -> 112
+    code, e, val = ox.quantize_blocks(np.array([[448.0, 1.0625, 1.1875, 17.0, 19.0]]))
+    assert val[0, 1:5].tolist() == [1.0, 1.25, 16.0, 20.0]                 # half way: to the even one
+
+
+def test_argument_errors_without_gpu():
+    """Non-null pointers are never dereferenced: every call fails in its checks."""
+    L, one, null = binding.lib(), ctypes.c_void_p(16), ctypes.c_void_p(0)
+    size = ctypes.c_size_t(7)
+    EINVAL, EDOMAIN = binding.SC_EINVAL, binding.SC_EDOMAIN
+    assert L.sc_route_workspace_bytes(10, 8, 2, None) == EINVAL
+    assert L.sc_route_workspace_bytes(-1, 8, 2, ctypes.byref(size)) == EINVAL
+    for n, k, t in ((10, 0, 1), (10, 4097, 1), (10, 8, 0), (10, 8, 9), (10, 64, 17), (2 ** 31, 8, 2)):
+        assert L.sc_route_workspace_bytes(n, k, t, ctypes.byref(size)) == EDOMAIN
+    assert L.sc_route_workspace_bytes(10, 8, 2, ctypes.byref(size)) == 0 and size.value > 0
+    need = size.value
+
+    def route(scores=one, dtype=0, ld=8, allowed=null, lda=0, n=10, k=8, t=2, out=one, work=one, wb=need):
+        return L.sc_route(scores, dtype, ld, allowed, lda, n, k, t, 1, out, out, out, out, out, work, wb, null)
+    assert route(scores=null) == EINVAL and route(out=null) == EINVAL and route(n=-1) == EINVAL and route(work=null) == EINVAL
+    assert route(dtype=3) == EDOMAIN and route(ld=7) == EDOMAIN and route(allowed=one, lda=7) == EDOMAIN
+    assert route(wb=need - 1) == EDOMAIN and route(t=0) == EDOMAIN
+
+    def back(scores=one, dtype=0, ld=8, n=10, k=8, t=2, norm=1, p=one, ldd=8):
+        return L.sc_route_backward(scores, dtype, ld, null, 0, n, k, t, norm, p, p, p, p, ldd, null)
+    assert back(p=null) == EINVAL and back(scores=null, norm=0) == EINVAL and back(ldd=7) == EDOMAIN and back(dtype=-1) == EDOMAIN
+    assert back(ld=7, norm=0) == EDOMAIN
+
+    def product(x=one, ldx=16, nx=4, w=one, ldw=16, ldg=0, dtype=1, off=one, order=one, slots=2, rows=8, groups=2, N=12, K=16, tr=0,
+                y=one, ldy=16):
+        return L.sc_grouped_product(x, ldx, nx, w, ldw, ldg, dtype, off, order, slots, rows, groups, N, K, tr, y, ldy, null)
+    for bad in (dict(x=null), dict(w=null), dict(off=null), dict(y=null), dict(rows=-1), dict(nx=-1)):
+        assert product(**bad) == EINVAL, bad
+    for bad in (dict(ldx=15), dict(ldw=15), dict(ldg=-1), dict(dtype=5), dict(slots=0), dict(groups=0), dict(N=0), dict(K=0),
+                dict(ldy=11), dict(rows=2 ** 31), dict(tr=1, ldx=11), dict(tr=1, ldy=15), dict(groups=2 ** 20 + 1)):
+        assert product(**bad) == EDOMAIN, bad
+
+    assert L.sc_grouped_gradient_workspace_bytes(8, 2, 12, 16, 1, None) == EINVAL
+    assert L.sc_grouped_gradient_workspace_bytes(8, 0, 12, 16, 1, ctypes.byref(size)) == EDOMAIN
+
+    def grad(dy=one, lddy=12, x=one, ldx=16, nx=4, dtype=1, off=one, slots=2, rows=8, groups=2, N=12, K=16, dw=one, ldw=16, ldg=192):
+        return L.sc_grouped_gradient(dy, lddy, x, ldx, nx, dtype, off, one, slots, rows, groups, N, K, dw, ldw, ldg, one, 1 << 30, null)
+    for bad in (dict(dy=null), dict(x=null), dict(off=null), dict(dw=null), dict(rows=-1)):
+        assert grad(**bad) == EINVAL, bad
+    for bad in (dict(lddy=11), dict(ldx=15), dict(ldw=15), dict(ldg=191), dict(dtype=9), dict(slots=0), dict(groups=0)):
+        assert grad(**bad) == EDOMAIN, bad
+
+    assert L.sc_group_combine(one, 1, 8, 8, null, null, 4, 2, 8, one, 8, null) == EINVAL
+    assert L.sc_group_combine(null, 1, 8, 8, one, null, 4, 2, 8, one, 8, null) == EINVAL
+    for dtype, ldz, t, d, ldo in ((7, 8, 2, 8, 8), (1, 7, 2, 8, 8), (1, 8, 0, 8, 8), (1, 8, 2, 0, 8), (1, 8, 2, 8, 7)):
+        assert L.sc_group_combine(one, dtype, ldz, 8, one, null, 4, t, d, one, ldo, null) == EDOMAIN
+    assert L.sc_group_combine_backward(one, 1, 8, null, 8, 8, one, one, one, 4, 2, 8, one, 8, one, null) == EINVAL
+    assert L.sc_group_combine_backward(one, 1, 8, one, 8, 8, one, one, one, 4, 2, 8, one, 7, one, null) == EDOMAIN
+
+    assert L.sc_quantize_blocks(null, 0, 200, 4, 200, one, 256, one, 2, null) == EINVAL
+    for dtype, ldx, K, ldq, lds in ((3, 200, 200, 256, 2), (0, 199, 200, 256, 2), (0, 200, 0, 256, 2), (0, 200, 200, 255, 2), (0, 200, 200, 256, 1)):
+        assert L.sc_quantize_blocks(one, dtype, ldx, 4, K, one, ldq, one, lds, null) == EDOMAIN
+        assert L.sc_dequantize_blocks(one, ldq, one, lds, 4, K, one, dtype, ldx, null) == EDOMAIN
+
+    def p8(x=one, ldx=256, w=one, ldw=256, ldg=2048, lds=2, off=one, dtype=1, N=8, K=200, y=one, ldy=8, slots=1):
+        return L.sc_grouped_product_e4m3(x, ldx, one, lds, 4, w, ldw, ldg, one, lds, 16, off, one, slots, 4, 2, N, K, dtype, y, ldy, null)
+    for bad in (dict(x=null), dict(w=null), dict(off=null), dict(y=null)):
+        assert p8(**bad) == EINVAL, bad
+    for bad in (dict(ldx=248), dict(ldw=240), dict(ldg=2047), dict(lds=1), dict(dtype=4), dict(N=0), dict(K=0), dict(ldy=7), dict(slots=0),
+                dict(x=ctypes.c_void_p(8)), dict(w=ctypes.c_void_p(24)), dict(K=2 ** 30 + 1)):
+        assert p8(**bad) == EDOMAIN, bad
+
+
+def test_empty_calls_need_no_gpu():
+    L, null, one = binding.lib(), ctypes.c_void_p(0), ctypes.c_void_p(16)
+    assert L.sc_group_combine(null, 1, 8, 0, null, null, 0, 2, 8, null, 8, null) == 0
+    assert L.sc_quantize_blocks(null, 0, 200, 0, 200, null, 256, null, 2, null) == 0
+    assert L.sc_grouped_product(null, 16, 0, one, 16, 0, 1, one, null, 1, 0, 2, 12, 16, 0, null, 16, null) == 0
