@@ -182,6 +182,425 @@ __global__ __launch_bounds__(256) void grouped_any_kernel(const T* __restrict__ 
   }
 }
 
+// ---- whole 16-byte pieces, 16-bit types --------------------------------------------------------------------------------------
+// A BM x BN tile by WR x WC waves.  The contraction goes through LDS in steps of 64, in five buffers that hold a step of one
+// operand each: while two are read, three are filled, the columns' operand two steps ahead and the rows' one and a half.  Pieces go
+// straight from memory into LDS.  An operand whose rows run along the contraction (`along`) lies in LDS row by row, 128 bytes
+// each, an operand whose rows run across it (`across`) step by step; the latter is turned by the transposing LDS read.
+// The 16-byte pieces of a row are permuted by the row's number, so that the rows (or steps)
+// that a read touches at once lie in different banks; as the loads write LDS in lane order it is the source address that is
+// permuted.
+__device__ uint4 zero_piece[1];
+
+typedef __attribute__((address_space(3))) void LdsVoid;
+typedef short short4v __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) short4v LdsShort4;
+
+// 16 bytes a lane from src to dst + 16 * lane, dst the same for the wave.  Written as an instruction of its own because the compiler
+// counts the builtin as an access that may return out of order and then waits for every LDS read at once; it returns nothing in a
+// register, and meet() waits for it.
+__device__ __forceinline__ void piece_to_lds(const void* src, void* dst) {
+  const uint32_t at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(LdsVoid*)dst);
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(at), "v"(src) : "memory");
+}
+__device__ __forceinline__ void arrived() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+// All pieces of all waves but the LEFT that each has asked for last are there, all LDS reads are done.
+template <int LEFT>
+__device__ __forceinline__ void meet() {
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LEFT) : "memory");
+}
+
+// All LDS reads of all waves so far are done.
+__device__ __forceinline__ void read_by_all() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+constexpr int kStep = 64;
+
+// How the pieces of a row change places: of a row of the rows' operand by the 16-byte piece, of the columns' operand too, but in
+// the order in which its fragments take the rows; of step e of an `across` operand by 32 bytes.
+__device__ __forceinline__ int row_shift(int r) { return r & 7; }
+__device__ __forceinline__ int col_shift(int c) { return ((c >> 3) & 3) | ((c << 1) & 4); }
+__device__ __forceinline__ int across_shift(int e) { return (e & 3) | ((e >> 1) & 4); }
+
+// Column (from the wave's first) of value i of column fragment b.  A lane gets values 4 q ... 4 q + 3 of every fragment (q = lane /
+// 16); so that those of two fragments are eight neighbours, one 16-byte store, the columns are dealt out in this order.
+__device__ __forceinline__ int fragment_col(int b, int i) { return (b >> 1) * 32 + (i >> 2) * 8 + (b & 1) * 4 + (i & 3); }
+
+template <typename T>
+__device__ __forceinline__ typename Matrix<T>::Chunk along_piece(const T* tile, int r, int shift, int piece) {
+  return *reinterpret_cast<const typename Matrix<T>::Chunk*>(tile + r * kStep + ((piece ^ shift) << 3));
+}
+// Values first + 0 ... 3 (this lane's part of the columns) of steps e and e + 4, turned.
+template <typename T, int EXT>
+__device__ __forceinline__ typename Matrix<T>::Chunk across_piece(const T* tile, int col, int e) {
+  union {
+    short4v part[2];
+    typename Matrix<T>::Chunk whole;
+  } u;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const T* p = tile + (e + 4 * h) * EXT + (((col >> 4) ^ across_shift(e + 4 * h)) << 4) + (col & 15);
+    u.part[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsShort4*)p);
+  }
+  return u.whole;
+}
+
+// Workgroups take one tile after the other: while the last two steps of a tile run, the first two of the next are fetched, and a
+// tile's results are stored while the next one's products run.  For that every tile has at least two steps, a gradient's three, as
+// the rows of x that a step takes are looked up a step before they are fetched; steps behind the contraction's end hold zeros.
+template <typename T, int FORM, int BM, int BN, int WR, int WC>
+__global__ __launch_bounds__(WR * WC * 64) void grouped_tile_kernel(
+    const T* __restrict__ rmat, const T* __restrict__ cmat, T* __restrict__ out, const int32_t* __restrict__ offsets,
+    const int32_t* __restrict__ order, int64_t ldr, int64_t ldc, int64_t ldg, int64_t ldo, int64_t ldog, int64_t rows,
+    int64_t xrows, int groups, int slots, int outr, int outc, int depth, int row_tiles, int col_tiles) {
+  typedef typename Matrix<T>::Chunk Chunk;
+  typedef T Part __attribute__((ext_vector_type(8)));
+  constexpr int NW = WR * WC;
+  constexpr int FR = BM / WR / 16, FC = BN / WC / 16;
+  constexpr bool R_ALONG = FORM != kGradient, C_ALONG = FORM == kProduct;
+  constexpr int LR = BM / 8 / NW, LC = BN / 8 / NW;  // loads of 1 KB a wave and step
+  static_assert(LR * 8 * NW == BM && LC * 8 * NW == BN && FR % 4 == 0 && FC % 2 == 0, "");
+  constexpr int BUFFERS = 5, BUFFER = (BM > BN ? BM : BN) * kStep;
+  __shared__ __attribute__((aligned(1024))) T lds[BUFFERS * BUFFER];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wr = wave / WC * (BM / WR), wc = wave % WC * (BN / WC);
+  const T* const zero = reinterpret_cast<const T*>(zero_piece);
+
+  // ---- the tiles ----
+  struct Tile {
+    int group, r0, rn, c0, cn;
+    int64_t pbegin;
+    int length;
+  };
+  const TileList<BM> list(offsets, FORM == kGradient ? 0 : groups, rows);
+  int64_t index, end;  // tiles of this workgroup: index, index + stride ... below end
+  int stride;
+  if (FORM == kGradient) {  // every die has a part of every group, as groups may be of very different length
+    index = blockIdx.x;
+    end = (int64_t)groups * row_tiles * col_tiles;
+    stride = gridDim.x;
+  } else {
+    // an eighth of the tiles to the workgroups of each die, neighbouring tiles at one time
+    const int64_t total = (int64_t)list.total * col_tiles, share = (total + 7) / 8;
+    stride = gridDim.x >> 3;
+    index = (int64_t)(blockIdx.x & 7) * share + (blockIdx.x >> 3);
+    end = min(total, (int64_t)((blockIdx.x & 7) + 1) * share);
+  }
+  auto tile_at = [&](int64_t i) {
+    Tile t;
+    if (FORM == kGradient) {
+      t.group = (int)(i / (row_tiles * col_tiles));
+      const int in = (int)(i - (int64_t)t.group * (row_tiles * col_tiles));
+      t.r0 = in / col_tiles * BM;
+      t.c0 = in % col_tiles * BN;
+      t.rn = min(BM, outr - t.r0);
+      const GroupRange g = group_range(offsets, groups, rows, t.group);
+      t.pbegin = g.begin;
+      t.length = (int)(g.end - g.begin);
+    } else {
+      const int row_tile = (int)(i / col_tiles);
+      const RowTile r = list.at(row_tile);
+      t.group = r.group;
+      t.r0 = 0;
+      t.rn = r.count;
+      t.pbegin = r.begin;
+      t.c0 = (int)(i - (int64_t)row_tile * col_tiles) * BN;
+      t.length = depth;
+    }
+    t.cn = min(BN, outc - t.c0);
+    return t;
+  };
+
+  // ---- what a lane loads ----
+  // `along` a fixed row, `across` a fixed column of its operand, and one step after the other of it.  Rows and columns outside the
+  // tile take the last one's values, which nothing stores; steps beyond the contraction's end come from a piece of zeros.
+  const T *rp[LR], *cp[LC];
+  const int along_r = lane >> 3;  // row within the eight that a load brings
+  int re[LR], ce[LC];
+#pragma unroll
+  for (int u = 0; u < LR; ++u) re[u] = R_ALONG ? ((lane & 7) ^ row_shift(along_r)) * 8
+                                               : (wave * LR + u) * (512 / BM) + lane / (BM / 8);
+#pragma unroll
+  for (int u = 0; u < LC; ++u) ce[u] = C_ALONG ? ((lane & 7) ^ col_shift((wave * LC + u) * 8 + along_r)) * 8
+                                               : (wave * LC + u) * (512 / BN) + lane / (BN / 8);
+  int32_t look[FORM == kGradient ? LC : LR];  // source rows: of the next tile, of the gradient's next step
+  auto look_up_rows = [&](const Tile& t) {
+    if (FORM != kGradient) {
+#pragma unroll
+      for (int u = 0; u < LR; ++u)
+        look[u] = (int32_t)source_row(order, t.pbegin + min((wave * LR + u) * 8 + along_r, t.rn - 1), slots, xrows);
+    }
+  };
+  auto look_up_step = [&](int64_t pbegin, int rest) {  // a step from grouped row pbegin on, `rest` rows are left
+    if (FORM == kGradient) {
+#pragma unroll
+      for (int u = 0; u < LC; ++u) look[u] = ce[u] < rest ? (int32_t)source_row(order, pbegin + ce[u], slots, xrows) : -1;
+    }
+  };
+  auto mask_rows = [&](int left) {  // the last step: what lies behind the end
+#pragma unroll
+    for (int u = 0; u < LR; ++u) rp[u] = re[u] < left ? rp[u] : zero;
+  };
+  auto mask_cols = [&](int left) {
+#pragma unroll
+    for (int u = 0; u < LC; ++u) cp[u] = ce[u] < left ? cp[u] : zero;
+  };
+  auto begin_rows = [&](const Tile& t) {
+#pragma unroll
+    for (int u = 0; u < LR; ++u) {
+      if (R_ALONG)
+        rp[u] = rmat + (look[u] < 0 ? 0 : look[u]) * ldr + re[u];
+      else
+        rp[u] = rmat + (t.pbegin + re[u]) * ldr + t.r0 + min((lane % (BM / 8) ^ (across_shift(re[u]) << 1)) * 8, t.rn - 8);
+    }
+    if (t.length < kStep) mask_rows(t.length);
+  };
+  auto col_of = [&](int c0, int cn, int u) { return c0 + min((lane % (BN / 8) ^ (across_shift(ce[u]) << 1)) * 8, cn - 8); };
+  auto step_cols = [&](int c0, int cn) {  // gradient: the rows that were looked up
+#pragma unroll
+    for (int u = 0; u < LC; ++u) cp[u] = look[u] < 0 ? zero : cmat + look[u] * ldc + col_of(c0, cn, u);
+  };
+  auto begin_cols = [&](const Tile& t) {
+    if (FORM == kGradient) {
+      step_cols(t.c0, t.cn);
+      return;
+    }
+    const T* base = cmat + (int64_t)t.group * ldg;
+#pragma unroll
+    for (int u = 0; u < LC; ++u) {
+      if (C_ALONG)
+        cp[u] = base + (int64_t)(t.c0 + min((wave * LC + u) * 8 + along_r, t.cn - 1)) * ldc + ce[u];
+      else
+        cp[u] = base + ce[u] * ldc + col_of(t.c0, t.cn, u);
+    }
+    if (t.length < kStep) mask_cols(t.length);
+  };
+  auto fetch_row = [&](int u, int buffer) { piece_to_lds(rp[u], lds + buffer * BUFFER + (wave * LR + u) * 512); };
+  auto fetch_col = [&](int u, int buffer) { piece_to_lds(cp[u], lds + buffer * BUFFER + (wave * LC + u) * 512); };
+
+  f32x4 acc[FR][FC];
+  auto clear = [&]() {
+#pragma unroll
+    for (int a = 0; a < FR; ++a)
+#pragma unroll
+      for (int b = 0; b < FC; ++b) acc[a][b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  };
+  int sub = lane & 15, quad = lane >> 4;
+  auto col_fragments = [&](int buffer, int kk, Chunk (&f)[FC]) {
+    const T* tile = lds + buffer * BUFFER;
+#pragma unroll
+    for (int b = 0; b < FC; ++b) {
+      if (C_ALONG) {
+        const int c = wc + fragment_col(b, sub);
+        f[b] = along_piece(tile, c, col_shift(c), kk * 4 + quad);
+      } else {
+        f[b] = across_piece<T, BN>(tile, wc + fragment_col(b, (sub & 3) * 4), kk * 32 + quad * 8 + (sub >> 2));
+      }
+    }
+  };
+  auto row_fragments = [&](int buffer, int kk, int pair, Chunk (&f)[2]) {
+    const T* tile = lds + buffer * BUFFER;
+#pragma unroll
+    for (int a = 0; a < 2; ++a) {
+      const int r = wr + (pair * 2 + a) * 16;
+      if (R_ALONG)
+        f[a] = along_piece(tile, r + sub, row_shift(r + sub), kk * 4 + quad);
+      else
+        f[a] = across_piece<T, BM>(tile, r + (sub & 3) * 4, kk * 32 + quad * 8 + (sub >> 2));
+    }
+  };
+  auto multiply = [&](int pair, const Chunk (&fr)[2], const Chunk (&fc)[FC]) {
+#pragma unroll
+    for (int a = 0; a < 2; ++a)
+#pragma unroll
+      for (int b = 0; b < FC; ++b) acc[pair * 2 + a][b] = Matrix<T>::mma(fc[b], fr[a], acc[pair * 2 + a][b]);
+  };
+  auto store = [&](const Tile& t) {
+    T* base = FORM == kGradient ? out + (int64_t)t.group * ldog + (int64_t)t.r0 * ldo : out + t.pbegin * ldo;
+    const int64_t known = xrows * slots;
+#pragma unroll
+    for (int a = 0; a < FR; ++a) {
+      const int row = wr + a * 16 + sub;
+      if (row >= t.rn) continue;
+      T* orow = base + row * ldo + t.c0;
+      const bool none = FORM != kGradient && order && (uint32_t)order[t.pbegin + row] >= known;  // a row of zeros
+#pragma unroll
+      for (int b = 0; b < FC; b += 2) {
+        const int col = wc + fragment_col(b, quad * 4);
+        if (col < t.cn) {  // widths are whole pieces
+          Part q;
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            q[u] = static_cast<T>(none ? 0.0f : acc[a][b][u]);
+            q[u + 4] = static_cast<T>(none ? 0.0f : acc[a][b + 1][u]);
+          }
+          *reinterpret_cast<Part*>(orow + col) = q;
+        }
+      }
+    }
+  };
+
+  // A step in two halves of PAIRS phases of two row fragments each; while a phase's products run the next one's values come out of
+  // LDS and a few loads are issued (all at once they hold the waves up for as long as they take to issue).  In the first half
+  // these are the columns' operand of the step after the next; in the second one, after a meeting behind which nobody reads this
+  // step's columns' operand any more, the rows' operand of that step into its place.  Before the last phase the waves meet again:
+  // there this step's rows' operand has been read by all as well, and all of the next step has arrived.
+  constexpr int PAIRS = FR / 2, CL = LC / PAIRS;
+  static_assert(CL * PAIRS == LC, "");
+  constexpr int EARLY = PAIRS > 2 ? LR / PAIRS * (PAIRS - 2) : 0;  // loads of the rows' operand before the second meeting
+  if (index < end) {
+    Tile tile = tile_at(index), next = tile;
+    clear();
+    Chunk fr[2][2], fc[2][FC];
+    constexpr int LEAST = FORM == kGradient ? 3 : 2;
+    auto steps_of = [&](const Tile& t) { return max(LEAST, (t.length + kStep - 1) / kStep); };
+    int left = steps_of(tile);                            // steps of this tile
+    int fleft = left, ftail = tile.length;                // steps and rest of the contraction where the pointers stand
+    int fc0 = tile.c0, fcn = tile.cn;                     // and its columns
+    int64_t lbegin = tile.pbegin;                         // the same where rows are looked up, a step further
+    int lleft = left, ltail = tile.length;
+    bool more;
+    auto look_further = [&]() {
+      if (FORM != kGradient) return;
+      if (--lleft > 0) {
+        lbegin += kStep;
+        ltail -= kStep;
+      } else if (more) {
+        lleft = steps_of(next);
+        lbegin = next.pbegin;
+        ltail = next.length;
+      } else {
+        lleft = 1;
+        ltail = 0;
+      }
+      look_up_step(lbegin, ltail);
+    };
+    auto advance = [&]() {
+      if (--fleft > 0) {
+        ftail -= kStep;
+#pragma unroll
+        for (int u = 0; u < LR; ++u) rp[u] += R_ALONG ? (int64_t)kStep : kStep * ldr;
+        if (FORM == kGradient) {
+          step_cols(fc0, fcn);
+        } else {
+#pragma unroll
+          for (int u = 0; u < LC; ++u) cp[u] += C_ALONG ? (int64_t)kStep : kStep * ldc;
+        }
+        if (ftail < kStep) {
+          mask_rows(ftail);
+          if (FORM != kGradient) mask_cols(ftail);
+        }
+      } else if (more) {
+        begin_rows(next);
+        begin_cols(next);
+        fleft = steps_of(next);
+        ftail = next.length;
+        fc0 = next.c0;
+        fcn = next.cn;
+      } else {  // nothing more: the same again, which nothing uses
+        fleft = 1;
+      }
+      look_further();
+    };
+    auto look_ahead = [&]() {
+      more = index + stride < end;
+      if (more) {
+        next = tile_at(index + stride);
+        look_up_rows(next);
+      }
+    };
+    int cnow = 0, rnow = 1, cnext = 2, rnext = 3, ahead = 4;  // buffers of this step, of the next one, and the free one
+    look_up_rows(tile);
+    look_up_step(lbegin, ltail);
+    begin_rows(tile);
+    begin_cols(tile);
+    look_ahead();
+    look_further();
+#pragma unroll
+    for (int f = 0; f < 2; ++f) {
+#pragma unroll
+      for (int u = 0; u < LC; ++u) fetch_col(u, f ? cnext : cnow);
+#pragma unroll
+      for (int u = 0; u < LR; ++u) fetch_row(u, f ? rnext : rnow);
+      advance();
+    }
+    meet<LR + LC>();
+    col_fragments(cnow, 0, fc[0]);
+    row_fragments(rnow, 0, 0, fr[0]);
+    for (;;) {
+      asm volatile("" : "+v"(sub), "+v"(quad));  // LDS addresses are made anew in every step: there are no registers to keep them
+#pragma unroll
+      for (int p = 0; p < PAIRS; ++p) {
+        __builtin_amdgcn_sched_barrier(0);
+        if (p + 1 < PAIRS) {
+          row_fragments(rnow, 0, p + 1, fr[(p + 1) & 1]);
+        } else {
+          col_fragments(cnow, 1, fc[1]);
+          row_fragments(rnow, 1, 0, fr[0]);
+        }
+#pragma unroll
+        for (int u = 0; u < CL; ++u) fetch_col(p * CL + u, ahead);
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_setprio(1);
+        multiply(p, fr[p & 1], fc[0]);
+        __builtin_amdgcn_s_setprio(0);
+      }
+#pragma unroll
+      for (int p = 0; p < PAIRS; ++p) {
+        __builtin_amdgcn_sched_barrier(0);
+        if (p == 1 && PAIRS > 2) read_by_all();
+        if (p + 1 < PAIRS) {
+          row_fragments(rnow, 1, p + 1, fr[(p + 1) & 1]);
+        } else {
+          meet<LC + EARLY>();
+          col_fragments(cnext, 0, fc[0]);
+          row_fragments(rnext, 0, 0, fr[0]);
+        }
+        if (p >= 1 && p + 1 < PAIRS) {
+#pragma unroll
+          for (int u = 0; u < LR / PAIRS; ++u) fetch_row((p - 1) * (LR / PAIRS) + u, cnow);
+        }
+        if (p + 1 == PAIRS) {
+#pragma unroll
+          for (int u = EARLY; u < LR; ++u) fetch_row(u, cnow);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_setprio(1);
+        multiply(p, fr[p & 1], fc[1]);
+        __builtin_amdgcn_s_setprio(0);
+      }
+      const int free = rnow, filled = cnow;
+      cnow = cnext;
+      rnow = rnext;
+      cnext = ahead;
+      rnext = filled;
+      ahead = free;
+      if (--left == 0) {
+        store(tile);
+        if (!more) break;
+        clear();
+        index += stride;
+        tile = next;
+        left = steps_of(tile);
+        look_ahead();
+      }
+      advance();
+    }
+    arrived();  // nothing may still be on its way into LDS when the workgroup gives it back
+  }
+
+  if (FORM != kGradient) {  // rows behind the last group
+    const GroupRange g = group_range(offsets, groups, rows, groups);
+    const int parts = outc / 8;
+    const int64_t count = (g.end - g.begin) * parts;
+    Part q;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) q[u] = static_cast<T>(0.0f);
+    for (int64_t i = (int64_t)blockIdx.x * (NW * 64) + tid; i < count; i += (int64_t)gridDim.x * (NW * 64))
+      *reinterpret_cast<Part*>(out + (g.begin + i / parts) * ldo + i % parts * 8) = q;
+  }
+}
+
 template <typename T>
 bool whole_chunks(const void* p, int64_t ld) {
   return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % Matrix<T>::kChunk == 0;
@@ -197,6 +616,21 @@ hipError_t product_typed(const GroupedArgs& a, bool transpose, hipStream_t st) {
   const int64_t blocks = tile_bound(a.rows, a.groups, kTile, cols);
   if (blocks > 0x7fffffff) return hipErrorInvalidConfiguration;
   const bool wide = whole_chunks<T>(a.x, a.ldx) && whole_chunks<T>(a.w, a.ldw) && a.ldg % CH == 0 && a.K % CH == 0 && a.N % CH == 0;
+  if constexpr (sizeof(T) == 2) {
+    if (wide && whole_chunks<T>(a.y, a.ldy)) {
+      constexpr int BM = 256, BN = 256;
+      const int wcols = (outc + BN - 1) / BN;
+      const int64_t n = tile_bound(a.rows, a.groups, BM, wcols);
+      const uint32_t grid = (uint32_t)(n < 256 ? n : 256);
+      if (transpose)
+        grouped_tile_kernel<T, kTransposed, BM, BN, 2, 4><<<grid, 512, 0, st>>>(
+            x, w, y, a.offsets, a.order, a.ldx, a.ldw, a.ldg, a.ldy, 0, a.rows, a.xrows, a.groups, a.slots, 0, outc, depth, 0, wcols);
+      else
+        grouped_tile_kernel<T, kProduct, BM, BN, 2, 4><<<grid, 512, 0, st>>>(
+            x, w, y, a.offsets, a.order, a.ldx, a.ldw, a.ldg, a.ldy, 0, a.rows, a.xrows, a.groups, a.slots, 0, outc, depth, 0, wcols);
+      return hipGetLastError();
+    }
+  }
 #define SC_LAUNCH(FORM, WIDE)                                                                                                   \
   grouped_any_kernel<T, FORM, WIDE><<<(uint32_t)blocks, 256, 0, st>>>(x, w, y, a.offsets, a.order, a.ldx, a.ldw, a.ldg, a.ldy, 0, \
                                                                       a.rows, a.xrows, a.groups, a.slots, 0, outc, depth, 0, cols)
@@ -217,6 +651,16 @@ hipError_t gradient_typed(const GradientArgs& a, hipStream_t st) {
   const int64_t blocks = (int64_t)a.groups * rt * ct;
   if (blocks > 0x7fffffff) return hipErrorInvalidConfiguration;
   const bool wide = whole_chunks<T>(a.x, a.ldx) && whole_chunks<T>(a.dy, a.lddy) && a.K % CH == 0 && a.N % CH == 0;
+  if constexpr (sizeof(T) == 2) {
+    if (wide && whole_chunks<T>(a.dw, a.ldw) && a.ldg % CH == 0) {
+      constexpr int BM = 256, BN = 256;
+      const int wr = (a.N + BM - 1) / BM, wc = (a.K + BN - 1) / BN;
+      const int64_t n = (int64_t)a.groups * wr * wc;
+      grouped_tile_kernel<T, kGradient, BM, BN, 2, 4><<<(uint32_t)(n < 256 ? n : 256), 512, 0, st>>>(
+          dy, x, dw, a.offsets, a.order, a.lddy, a.ldx, 0, a.ldw, a.ldg, a.rows, a.xrows, a.groups, a.slots, a.N, a.K, 0, wr, wc);
+      return hipGetLastError();
+    }
+  }
 #define SC_LAUNCH(WIDE)                                                                                                        \
   grouped_any_kernel<T, kGradient, WIDE><<<(uint32_t)blocks, 256, 0, st>>>(dy, x, dw, a.offsets, a.order, a.lddy, a.ldx, 0, a.ldw, \
                                                                            a.ldg, a.rows, a.xrows, a.groups, a.slots, a.N, a.K, 0, \

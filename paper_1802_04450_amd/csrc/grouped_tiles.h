@@ -80,6 +80,55 @@ __device__ __forceinline__ RowTile find_tile(const int32_t* offsets, int groups,
   return t;
 }
 
+// The same for workgroups that take one tile after the other: the row tiles of all groups are numbered in order.
+template <int BM>
+struct TileList {
+  const int32_t* offsets;
+  int64_t rows;
+  int groups, per, mine, sum;
+  int total;  // row tiles
+
+  __device__ __forceinline__ TileList(const int32_t* o, int g, int64_t r) : offsets(o), rows(r), groups(g) {
+    const int lane = threadIdx.x & 63;
+    per = (groups + 63) / 64;
+    mine = 0;
+    for (int u = 0; u < per; ++u) {
+      if (lane * per + u >= groups) break;
+      const GroupRange r2 = group_range(offsets, groups, rows, lane * per + u);
+      mine += (int)((r2.end - r2.begin + BM - 1) / BM);
+    }
+    sum = mine;
+#pragma unroll
+    for (int s = 1; s < 64; s <<= 1) {
+      const int v = __shfl_up(sum, s);
+      if (lane >= s) sum += v;
+    }
+    total = __builtin_amdgcn_readlane(sum, 63);
+  }
+  __device__ __forceinline__ RowTile at(int row_tile) const {  // 0 <= row_tile < total
+    RowTile t;
+    const uint64_t has = __ballot(row_tile < sum);
+    const int owner = __ffsll((unsigned long long)has) - 1;
+    int left = row_tile - __builtin_amdgcn_readlane(sum - mine, owner);
+    t.group = 0;
+    t.begin = 0;
+    t.count = 0;
+    t.col = 0;
+    for (int g = owner * per; g < groups; ++g) {
+      const GroupRange r = group_range(offsets, groups, rows, g);
+      const int tiles = (int)((r.end - r.begin + BM - 1) / BM);
+      if (left < tiles) {
+        t.group = g;
+        t.begin = r.begin + (int64_t)left * BM;
+        t.count = (int)min(r.end - t.begin, (int64_t)BM);
+        break;
+      }
+      left -= tiles;
+    }
+    return t;
+  }
+};
+
 // Workgroups that find_tile needs at most: every group adds at most one tile that is not full, and no tile is without a row.
 inline int64_t tile_bound(int64_t rows, int groups, int bm, int64_t cols) {
   const int64_t full = rows / bm + groups + 1;
