@@ -337,6 +337,288 @@ __global__ __launch_bounds__(256) void e4m3_wide_kernel(E4m3Args a, int cols) {
   }
 }
 
+// ---- product, 256 x 256 ---------------------------------------------------------------------------------------------------
+// Eight waves, 128 x 64 of the tile each.  A step is one block of the contraction, 128 bytes of every row; it goes through LDS as the
+// 16-bit products' steps do (five buffers that hold a step of one operand, pieces straight from memory, the columns' operand two
+// steps ahead, the rows' one and a half; workgroups that take one tile after the other).  The instructions are the 32 x 32 x 64 ones:
+// a lane holds 32 bytes of one row, two pieces of its half of the step, and as all of them belong to one block every lane of a
+// row hands over the same power of two.  Those come four steps at a time as one word a row, shifted by a byte a step.
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+__device__ __forceinline__ int piece_shift(int r) { return (r >> 1) & 7; }
+// Column of value i of a column fragment: bits 2 and 3 change places, so that a lane's eight values of two neighbouring groups of
+// four are eight neighbours.
+__device__ __forceinline__ int fragment_col(int i) { return (i & 0x13) | ((i & 4) << 1) | ((i & 8) >> 1); }
+
+template <typename T>
+__global__ __launch_bounds__(512) void e4m3_tile_kernel(E4m3Args a, int col_tiles, int whole_stores) {
+  constexpr int BM = 256, BN = 256, WC = 4, NW = 8, FR = 4, FC = 2, LOADS = 4;
+  constexpr int BUFFER = BM * kScaleBlock;
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[5 * BUFFER];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wr = wave / WC * (FR * 32), wc = wave % WC * (FC * 32);
+  struct Tile {
+    int group, rn, c0, cn;
+    int64_t pbegin;
+  };
+  const TileList<BM> list(a.offsets, a.groups, a.rows);
+  const int64_t total = (int64_t)list.total * col_tiles, share = (total + 7) / 8;
+  const int stride = gridDim.x >> 3;
+  int64_t index = (int64_t)(blockIdx.x & 7) * share + (blockIdx.x >> 3);
+  const int64_t end = min(total, (int64_t)((blockIdx.x & 7) + 1) * share);
+  auto tile_at = [&](int64_t i) {
+    const int row_tile = (int)(i / col_tiles);
+    const RowTile r = list.at(row_tile);
+    Tile t;
+    t.group = r.group;
+    t.rn = r.count;
+    t.pbegin = r.begin;
+    t.c0 = (int)(i - (int64_t)row_tile * col_tiles) * BN;
+    t.cn = min(BN, a.N - t.c0);
+    return t;
+  };
+  const int steps = a.Kp / kScaleBlock;
+
+  // Where a lane's pieces come from, in bytes from x and from the group's matrix (below 2^32, the launch sees to that).
+  const __amdgpu_buffer_rsrc_t xres =
+      __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(a.x), 0, (int)(uint32_t)(a.xrows * a.ldx), 0x00027000);
+  __amdgpu_buffer_rsrc_t wres = xres;
+  uint32_t ro[LOADS], co[LOADS];
+  const int eight = lane >> 3;
+  int32_t look[LOADS], looks[FR];  // source rows of the next tile: that the lane loads, whose scales it needs
+  const uint8_t *xsp[FR], *wsp[FC];
+  int sub = lane & 31, half = lane >> 5;
+  auto look_up = [&](const Tile& t) {
+#pragma unroll
+    for (int u = 0; u < LOADS; ++u)
+      look[u] = (int32_t)source_row(a.order, t.pbegin + min((wave * LOADS + u) * 8 + eight, t.rn - 1), a.slots, a.xrows);
+#pragma unroll
+    for (int f = 0; f < FR; ++f)
+      looks[f] = (int32_t)source_row(a.order, t.pbegin + min(wr + f * 32 + (lane & 31), t.rn - 1), a.slots, a.xrows);
+  };
+  auto begin = [&](const Tile& t) {
+#pragma unroll
+    for (int u = 0; u < LOADS; ++u) {
+      const int r = (wave * LOADS + u) * 8 + eight;
+      const int piece = ((lane & 7) ^ piece_shift(r)) * 16;
+      ro[u] = (uint32_t)(max(look[u], 0) * a.ldx + piece);
+      co[u] = (uint32_t)((int64_t)(t.c0 + min(r, t.cn - 1)) * a.ldw + piece);
+    }
+    wres = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(a.w) + (int64_t)t.group * a.ldg, 0,
+                                             (int)(uint32_t)((int64_t)(a.N - 1) * a.ldw + a.Kp), 0x00027000);
+  };
+  auto begin_scales = [&](const Tile& t) {
+#pragma unroll
+    for (int f = 0; f < FR; ++f) xsp[f] = a.xs + max(looks[f], 0) * a.ldxs;
+#pragma unroll
+    for (int f = 0; f < FC; ++f)
+      wsp[f] = a.ws + (int64_t)t.group * a.ldgs + (int64_t)(t.c0 + min(wc + f * 32 + fragment_col(lane & 31), t.cn - 1)) * a.ldws;
+  };
+  // The scales of steps b ... b + 3 in the low bytes after a shift by scale_shift(b): a word that ends with the row's last scale.
+  auto scale_word = [&](const uint8_t* p, int b) -> uint32_t {
+    uint32_t w;
+    if (steps >= 4) {
+      __builtin_memcpy(&w, p + min(b, steps - 4), 4);
+    } else {
+      w = p[0] | (uint32_t)p[1] << 8;
+      if (steps > 2) w |= (uint32_t)p[2] << 16;
+    }
+    return w;
+  };
+  auto scale_shift = [&](int b) { return steps >= 4 ? 8 * (b - min(b, steps - 4)) : 0; };
+  auto fetch_row = [&](int u, int buffer, int at) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(xres, (LdsVoid*)(lds + buffer * BUFFER + (wave * LOADS + u) * 1024), 16, ro[u], at, 0, 0);
+  };
+  auto fetch_col = [&](int u, int buffer, int at) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(wres, (LdsVoid*)(lds + buffer * BUFFER + (wave * LOADS + u) * 1024), 16, co[u], at, 0, 0);
+  };
+
+  f32x16 acc[FR][FC];
+  auto clear = [&]() {
+#pragma unroll
+    for (int f = 0; f < FR; ++f)
+#pragma unroll
+      for (int c = 0; c < FC; ++c)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[f][c][i] = 0.0f;
+  };
+  auto fragment = [&](int buffer, int r, int kk, i32x8& f) {
+    const uint8_t* row = lds + buffer * BUFFER + r * kScaleBlock;
+    const int shift = piece_shift(r);
+    const i32x4 p = *reinterpret_cast<const i32x4*>(row + (((kk * 4 + half) ^ shift) << 4));
+    const i32x4 q = *reinterpret_cast<const i32x4*>(row + (((kk * 4 + 2 + half) ^ shift) << 4));
+    f = __builtin_shufflevector(p, q, 0, 1, 2, 3, 4, 5, 6, 7);
+  };
+  auto col_fragments = [&](int buffer, int kk, i32x8 (&f)[FC]) {
+#pragma unroll
+    for (int c = 0; c < FC; ++c) fragment(buffer, wc + c * 32 + fragment_col(sub), kk, f[c]);
+  };
+  auto row_fragment = [&](int buffer, int kk, int r, i32x8& f) { fragment(buffer, wr + r * 32 + sub, kk, f); };
+  auto store = [&](const Tile& t) {
+    T* base = static_cast<T*>(a.y) + t.pbegin * a.ldy + t.c0;
+    const int64_t known = a.xrows * a.slots;
+    typedef T Part __attribute__((ext_vector_type(8)));
+#pragma unroll
+    for (int f = 0; f < FR; ++f) {
+      const int row = wr + f * 32 + (lane & 31);
+      if (row >= t.rn) continue;
+      const bool none = a.order && (uint32_t)a.order[t.pbegin + row] >= known;  // a row of zeros
+#pragma unroll
+      for (int c = 0; c < FC; ++c)
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+          const int col = wc + c * 32 + g * 16 + (lane >> 5) * 8;
+          T* out = base + row * a.ldy + col;
+          Part q;
+#pragma unroll
+          for (int u = 0; u < 8; ++u) q[u] = static_cast<T>(none ? 0.0f : acc[f][c][g * 8 + u]);
+          if (whole_stores) {
+            if (col < t.cn) *reinterpret_cast<Part*>(out) = q;
+          } else {
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+              if (col + u < t.cn) out[u] = q[u];
+          }
+        }
+    }
+  };
+
+  if (index < end) {
+    Tile tile = tile_at(index), next = tile;
+    clear();
+    i32x8 fr[2], fc[2][FC];
+    uint32_t xw[FR], ww[FC], xn[FR], wn[FC];  // scales of this and the next four steps
+    bool more;
+    int done = 0, at = 0;  // steps of the tile that are done; where the loads stand, in bytes along the contraction
+    auto look_ahead = [&]() {
+      more = index + stride < end;
+      if (more) {
+        next = tile_at(index + stride);
+        look_up(next);
+      }
+    };
+    auto advance = [&]() {
+      at += kScaleBlock;
+      if (at == a.Kp && more) {
+        begin(next);
+        at = 0;
+      } else if (at == a.Kp) {
+        at = 0;  // nothing more: what is fetched is there, and nothing uses it
+      }
+    };
+    auto scales = [&](int b) {
+#pragma unroll
+      for (int f = 0; f < FR; ++f) xn[f] = scale_word(xsp[f], b);
+#pragma unroll
+      for (int f = 0; f < FC; ++f) wn[f] = scale_word(wsp[f], b);
+    };
+    auto take_scales = [&](int b) {
+      const int shift = scale_shift(b);
+#pragma unroll
+      for (int f = 0; f < FR; ++f) xw[f] = xn[f] >> shift;
+#pragma unroll
+      for (int f = 0; f < FC; ++f) ww[f] = wn[f] >> shift;
+    };
+    auto multiply = [&](int r, const i32x8& f, const i32x8 (&c)[FC]) {
+#pragma unroll
+      for (int u = 0; u < FC; ++u)
+        acc[r][u] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(c[u], f, acc[r][u], 0, 0, 0, ww[u], 0, xw[r]);
+    };
+    int cnow = 0, rnow = 1, cnext = 2, rnext = 3, ahead = 4;  // buffers of this step, of the next one, and the free one
+    look_up(tile);
+    begin(tile);
+    begin_scales(tile);
+    scales(0);
+    take_scales(0);
+    look_ahead();
+#pragma unroll
+    for (int f = 0; f < 2; ++f) {
+#pragma unroll
+      for (int u = 0; u < LOADS; ++u) fetch_col(u, f ? cnext : cnow, at);
+#pragma unroll
+      for (int u = 0; u < LOADS; ++u) fetch_row(u, f ? rnext : rnow, at);
+      advance();
+    }
+    meet<2 * LOADS>();
+    col_fragments(cnow, 0, fc[0]);
+    row_fragment(rnow, 0, 0, fr[0]);
+    for (;;) {
+      asm volatile("" : "+v"(sub), "+v"(half));  // LDS addresses are made anew in every step: there are no registers to keep them
+      if ((done & 3) == 0 && done + 4 < steps) scales(done + 4);
+#pragma unroll
+      for (int p = 0; p < FR; ++p) {
+        __builtin_amdgcn_sched_barrier(0);
+        if (p + 1 < FR) {
+          row_fragment(rnow, 0, p + 1, fr[(p + 1) & 1]);
+        } else {
+          col_fragments(cnow, 1, fc[1]);
+          row_fragment(rnow, 1, 0, fr[0]);
+        }
+        fetch_col(p, ahead, at);
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_setprio(1);
+        multiply(p, fr[p & 1], fc[0]);
+        __builtin_amdgcn_s_setprio(0);
+      }
+#pragma unroll
+      for (int p = 0; p < FR; ++p) {
+        __builtin_amdgcn_sched_barrier(0);
+        if (p == 1) read_by_all();
+        if (p + 1 < FR) {
+          row_fragment(rnow, 1, p + 1, fr[(p + 1) & 1]);
+        } else {
+          meet<LOADS + 2>();
+          col_fragments(cnext, 0, fc[0]);
+          row_fragment(rnext, 0, 0, fr[0]);
+        }
+        if (p == 1 || p == 2) fetch_row(p - 1, cnow, at);
+        if (p == 3) {
+          fetch_row(2, cnow, at);
+          fetch_row(3, cnow, at);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_setprio(1);
+        multiply(p, fr[p & 1], fc[1]);
+        __builtin_amdgcn_s_setprio(0);
+      }
+      const int free = rnow, filled = cnow;
+      cnow = cnext;
+      rnow = rnext;
+      cnext = ahead;
+      rnext = filled;
+      ahead = free;
+      ++done;
+      if (done == steps) {
+        store(tile);
+        if (!more) break;
+        clear();
+        index += stride;
+        tile = next;
+        begin_scales(tile);
+        done = 0;
+        scales(0);
+        take_scales(0);
+        look_ahead();
+      } else if ((done & 3) == 0) {
+        take_scales(done);
+      } else {
+#pragma unroll
+        for (int f = 0; f < FR; ++f) xw[f] >>= 8;
+#pragma unroll
+        for (int f = 0; f < FC; ++f) ww[f] >>= 8;
+      }
+      advance();
+    }
+    arrived();  // nothing may still be on its way into LDS when the workgroup gives it back
+  }
+  // rows behind the last group
+  const GroupRange g = group_range(a.offsets, a.groups, a.rows, a.groups);
+  const int64_t count = (g.end - g.begin) * a.N;
+  for (int64_t i = (int64_t)blockIdx.x * (NW * 64) + tid; i < count; i += (int64_t)gridDim.x * (NW * 64))
+    static_cast<T*>(a.y)[(g.begin + i / a.N) * a.ldy + i % a.N] = static_cast<T>(0.0f);
+}
+
 template <typename T>
 hipError_t quantize_typed(const T* x, int64_t ldx, int64_t rows, int K, uint8_t* q, int64_t ldq, uint8_t* scale, int64_t lds,
                           hipStream_t st) {
@@ -366,6 +648,16 @@ hipError_t product_typed(const E4m3Args& a, hipStream_t st) {
   const int cols = (a.N + kTile - 1) / kTile;
   const int64_t blocks = tile_bound(a.rows, a.groups, kTile, cols);
   if (blocks > 0x7fffffff) return hipErrorInvalidConfiguration;
+  if constexpr (sizeof(T) == 2) {
+    // two steps at least, and offsets of 32 bits
+    if (a.Kp >= 2 * kScaleBlock && a.xrows * a.ldx < (int64_t)1 << 32 && a.N * a.ldw < (int64_t)1 << 32) {
+      const int wcols = (a.N + 255) / 256;
+      const int64_t n = tile_bound(a.rows, a.groups, 256, wcols);
+      const int whole = a.N % 8 == 0 && a.ldy % 8 == 0 && reinterpret_cast<uintptr_t>(a.y) % 16 == 0;
+      e4m3_tile_kernel<T><<<(uint32_t)(n < 256 ? n : 256), 512, 0, st>>>(a, wcols, whole);
+      return hipGetLastError();
+    }
+  }
   if constexpr (sizeof(T) == 4)
     e4m3_wide_kernel<<<(uint32_t)blocks, 256, 0, st>>>(a, cols);
   else

@@ -192,7 +192,6 @@ __global__ __launch_bounds__(256) void grouped_any_kernel(const T* __restrict__ 
 // permuted.
 __device__ uint4 zero_piece[1];
 
-typedef __attribute__((address_space(3))) void LdsVoid;
 typedef short short4v __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) short4v LdsShort4;
 
@@ -203,16 +202,6 @@ __device__ __forceinline__ void piece_to_lds(const void* src, void* dst) {
   const uint32_t at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(LdsVoid*)dst);
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(at), "v"(src) : "memory");
 }
-__device__ __forceinline__ void arrived() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
-// All pieces of all waves but the LEFT that each has asked for last are there, all LDS reads are done.
-template <int LEFT>
-__device__ __forceinline__ void meet() {
-  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LEFT) : "memory");
-}
-
-// All LDS reads of all waves so far are done.
-__device__ __forceinline__ void read_by_all() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
-
 constexpr int kStep = 64;
 
 // How the pieces of a row change places: of a row of the rows' operand by the 16-byte piece, of the columns' operand too, but in

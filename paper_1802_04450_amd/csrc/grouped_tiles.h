@@ -136,6 +136,17 @@ inline int64_t tile_bound(int64_t rows, int groups, int bm, int64_t cols) {
   return (tiles + 7) / 8 * 8;
 }
 
+typedef __attribute__((address_space(3))) void LdsVoid;
+__device__ __forceinline__ void arrived() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+// All pieces of all waves but the LEFT that each has asked for last are there, all LDS reads are done.
+template <int LEFT>
+__device__ __forceinline__ void meet() {
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LEFT) : "memory");
+}
+
+// All LDS reads of all waves so far are done.
+__device__ __forceinline__ void read_by_all() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
 // Source row of row p of a group, or -1: what `order` holds beyond [0, xrows * slots) reads as a row of zeros.
 __device__ __forceinline__ int64_t source_row(const int32_t* order, int64_t p, int slots, int64_t xrows) {
   const int64_t r = order ? (order[p] < 0 ? -1 : (int64_t)((uint32_t)order[p] / (uint32_t)slots)) : p;
