@@ -516,11 +516,26 @@ def sc_knn_union_pairs(idx, dist, sigma: float = 0.0):
 SC_F32, SC_BF16, SC_F16 = 0, 1, 2
 
 
+_kinds = {}
+
+
 def _dtype(t) -> int:
+    if not _kinds:
+        import torch
+        _kinds.update({torch.float32: SC_F32, torch.bfloat16: SC_BF16, torch.float16: SC_F16})
+    assert t in _kinds, t
+    return _kinds[t]
+
+
+def _enqueue(device, call, *args) -> None:
+    """One of the calls below on the current stream of `device`.  They take a few microseconds, so that what the context manager
+    and the stream object cost (5 us) is left out where the device is the current one."""
     import torch
-    kinds = {torch.float32: SC_F32, torch.bfloat16: SC_BF16, torch.float16: SC_F16}
-    assert t in kinds, t
-    return kinds[t]
+    if torch.cuda.current_device() == device.index:
+        _check(call(*args, torch._C._cuda_getCurrentRawStream(device.index)))
+    else:
+        with torch.cuda.device(device):
+            _check(call(*args, torch._C._cuda_getCurrentRawStream(device.index)))
 
 
 def _matrix(t, device=None):
@@ -573,11 +588,8 @@ def sc_route(scores, t: int, allowed=None, normalize: bool = True):
     need = ctypes.c_size_t(0)
     _check(lib().sc_route_workspace_bytes(n, k, t, ctypes.byref(need)))
     work = torch.empty(need.value, dtype=torch.uint8, device=dev)
-    with torch.cuda.device(dev):
-        code = lib().sc_route(_ptr(scores), _dtype(scores.dtype), _ld(scores), _ptr(allowed), lda, n, k, t, int(normalize),
-                              _ptr(idx), _ptr(weight), _ptr(offsets), _ptr(order), _ptr(place), _ptr(work), need.value,
-                              _stream())
-    _check(code)
+    _enqueue(dev, lib().sc_route, _ptr(scores), _dtype(scores.dtype), _ld(scores), _ptr(allowed), lda, n, k, t,
+             int(normalize), _ptr(idx), _ptr(weight), _ptr(offsets), _ptr(order), _ptr(place), _ptr(work), need.value)
     return idx, weight, offsets, order, place
 
 
@@ -592,10 +604,8 @@ def sc_route_backward(scores, idx, weight, dweight, allowed=None, normalize: boo
     _ints(idx, n * t, dev), _dev(weight, torch.float32), _dev(dweight, torch.float32)
     assert weight.shape == idx.shape == dweight.shape, (weight.shape, idx.shape, dweight.shape)
     out = torch.empty((n, k), dtype=scores.dtype, device=dev)
-    with torch.cuda.device(dev):
-        code = lib().sc_route_backward(_ptr(scores), _dtype(scores.dtype), _ld(scores), _ptr(allowed), lda, n, k, t,
-                                       int(normalize), _ptr(idx), _ptr(weight), _ptr(dweight), _ptr(out), k, _stream())
-    _check(code)
+    _enqueue(dev, lib().sc_route_backward, _ptr(scores), _dtype(scores.dtype), _ld(scores), _ptr(allowed), lda, n, k, t,
+             int(normalize), _ptr(idx), _ptr(weight), _ptr(dweight), _ptr(out), k)
     return out
 
 
@@ -615,11 +625,8 @@ def sc_grouped_product(x, w, offsets, order=None, slots: int = 1, transpose: boo
     if out is None:
         out = torch.empty((rows, cols), dtype=x.dtype, device=dev)
     assert _matrix(out, dev).shape == (rows, cols) and out.dtype == x.dtype, (out.shape, out.dtype)
-    with torch.cuda.device(dev):
-        code = lib().sc_grouped_product(_ptr(x), _ld(x), x.shape[0], _ptr(w), _ld(w, 1), _ld(w), _dtype(x.dtype),
-                                        _ptr(offsets), _ptr(order), slots, rows, groups, N, K, int(transpose), _ptr(out),
-                                        _ld(out), _stream())
-    _check(code)
+    _enqueue(dev, lib().sc_grouped_product, _ptr(x), _ld(x), x.shape[0], _ptr(w), _ld(w, 1), _ld(w), _dtype(x.dtype),
+             _ptr(offsets), _ptr(order), slots, rows, groups, N, K, int(transpose), _ptr(out), _ld(out))
     return out
 
 
@@ -642,11 +649,9 @@ def sc_grouped_gradient(dy, x, offsets, order=None, slots: int = 1, out=None):
     need = ctypes.c_size_t(0)
     _check(lib().sc_grouped_gradient_workspace_bytes(rows, groups, N, K, _dtype(dy.dtype), ctypes.byref(need)))
     work = torch.empty(need.value, dtype=torch.uint8, device=dev)
-    with torch.cuda.device(dev):
-        code = lib().sc_grouped_gradient(_ptr(dy), _ld(dy), _ptr(x), _ld(x), x.shape[0], _dtype(dy.dtype), _ptr(offsets),
-                                         _ptr(order), slots, rows, groups, N, K, _ptr(out), _ld(out, 1), _ld(out),
-                                         _ptr(work), need.value, _stream())
-    _check(code)
+    _enqueue(dev, lib().sc_grouped_gradient, _ptr(dy), _ld(dy), _ptr(x), _ld(x), x.shape[0], _dtype(dy.dtype),
+             _ptr(offsets), _ptr(order), slots, rows, groups, N, K, _ptr(out), _ld(out, 1), _ld(out), _ptr(work),
+             need.value)
     return out
 
 
@@ -662,10 +667,8 @@ def sc_group_combine(z, place, weight=None):
         assert _dev(weight, torch.float32).shape == place.shape and weight.device == dev, (weight.shape, place.shape)
     rows, d = z.shape
     out = torch.empty((n, d), dtype=z.dtype, device=dev)
-    with torch.cuda.device(dev):
-        code = lib().sc_group_combine(_ptr(z), _dtype(z.dtype), _ld(z), rows, _ptr(place), _ptr(weight), n, t, d, _ptr(out),
-                                      max(d, 1), _stream())
-    _check(code)
+    _enqueue(dev, lib().sc_group_combine, _ptr(z), _dtype(z.dtype), _ld(z), rows, _ptr(place), _ptr(weight), n, t, d,
+             _ptr(out), max(d, 1))
     return out
 
 
@@ -683,11 +686,8 @@ def sc_group_combine_backward(dout, z, place, weight, order):
         assert _dev(weight, torch.float32).shape == place.shape and weight.device == dev, (weight.shape, place.shape)
         dweight = torch.empty((n, t), dtype=torch.float32, device=dev)
     dz = torch.empty((rows, d), dtype=z.dtype, device=dev)
-    with torch.cuda.device(dev):
-        code = lib().sc_group_combine_backward(_ptr(dout), _dtype(z.dtype), _ld(dout), _ptr(z), _ld(z), rows, _ptr(place),
-                                               _ptr(weight), _ptr(order), n, t, d, _ptr(dz), max(d, 1), _ptr(dweight),
-                                               _stream())
-    _check(code)
+    _enqueue(dev, lib().sc_group_combine_backward, _ptr(dout), _dtype(z.dtype), _ld(dout), _ptr(z), _ld(z), rows,
+             _ptr(place), _ptr(weight), _ptr(order), n, t, d, _ptr(dz), max(d, 1), _ptr(dweight))
     return dz, dweight
 
 
@@ -700,10 +700,8 @@ def sc_quantize_blocks(x):
     rows, blocks = x2.shape[0], -(-K // 128)
     q = torch.empty((*x.shape[:-1], blocks * 128), dtype=torch.float8_e4m3fn, device=x.device)
     scale = torch.empty((*x.shape[:-1], blocks), dtype=torch.uint8, device=x.device)
-    with torch.cuda.device(x.device):
-        code = lib().sc_quantize_blocks(_ptr(x2), _dtype(x.dtype), _ld(x2), rows, K, _ptr(q), blocks * 128, _ptr(scale),
-                                        blocks, _stream())
-    _check(code)
+    _enqueue(x.device, lib().sc_quantize_blocks, _ptr(x2), _dtype(x.dtype), _ld(x2), rows, K, _ptr(q), blocks * 128,
+             _ptr(scale), blocks)
     return q, scale
 
 
@@ -721,10 +719,8 @@ def sc_dequantize_blocks(q, scale, K: Optional[int] = None, dtype=None):
     K = q.shape[-1] if K is None else K
     assert q.shape[-1] - 128 < K <= q.shape[-1], (K, q.shape)
     out = torch.empty((*q.shape[:-1], K), dtype=dtype or torch.float32, device=q.device)
-    with torch.cuda.device(q.device):
-        code = lib().sc_dequantize_blocks(_ptr(q), q.shape[-1], _ptr(scale), scale.shape[-1], out.numel() // K, K, _ptr(out),
-                                          _dtype(out.dtype), K, _stream())
-    _check(code)
+    _enqueue(q.device, lib().sc_dequantize_blocks, _ptr(q), q.shape[-1], _ptr(scale), scale.shape[-1], out.numel() // K,
+             K, _ptr(out), _dtype(out.dtype), K)
     return out
 
 
@@ -741,11 +737,9 @@ def sc_grouped_product_e4m3(xq, xscale, wq, wscale, offsets, order=None, slots: 
     if out is None:
         out = torch.empty((rows, N), dtype=dtype or torch.bfloat16, device=dev)
     assert _matrix(out, dev).shape == (rows, N), out.shape
-    with torch.cuda.device(dev):
-        code = lib().sc_grouped_product_e4m3(_ptr(xq), Kp, _ptr(xscale), Kp // 128, xq.shape[0], _ptr(wq), Kp, N * Kp,
-                                             _ptr(wscale), Kp // 128, N * (Kp // 128), _ptr(offsets), _ptr(order), slots,
-                                             rows, groups, N, Kp, _dtype(out.dtype), _ptr(out), _ld(out), _stream())
-    _check(code)
+    _enqueue(dev, lib().sc_grouped_product_e4m3, _ptr(xq), Kp, _ptr(xscale), Kp // 128, xq.shape[0], _ptr(wq), Kp, N *
+             Kp, _ptr(wscale), Kp // 128, N * (Kp // 128), _ptr(offsets), _ptr(order), slots, rows, groups, N, Kp,
+             _dtype(out.dtype), _ptr(out), _ld(out))
     return out
 
 

@@ -362,19 +362,14 @@ __global__ __launch_bounds__(512) void e4m3_tile_kernel(E4m3Args a, int col_tile
     int group, rn, c0, cn;
     int64_t pbegin;
   };
-  const TileList<BM> list(a.offsets, a.groups, a.rows);
-  const int64_t total = (int64_t)list.total * col_tiles, share = (total + 7) / 8;
-  const int stride = gridDim.x >> 3;
-  int64_t index = (int64_t)(blockIdx.x & 7) * share + (blockIdx.x >> 3);
-  const int64_t end = min(total, (int64_t)((blockIdx.x & 7) + 1) * share);
+  const TileWalk<BM> walk(a.offsets, a.groups, a.rows, col_tiles);
   auto tile_at = [&](int64_t i) {
-    const int row_tile = (int)(i / col_tiles);
-    const RowTile r = list.at(row_tile);
+    const RowTile r = walk.at(i);
     Tile t;
     t.group = r.group;
     t.rn = r.count;
     t.pbegin = r.begin;
-    t.c0 = (int)(i - (int64_t)row_tile * col_tiles) * BN;
+    t.c0 = r.col * BN;
     t.cn = min(BN, a.N - t.c0);
     return t;
   };
@@ -484,17 +479,18 @@ __global__ __launch_bounds__(512) void e4m3_tile_kernel(E4m3Args a, int col_tile
     }
   };
 
-  if (index < end) {
-    Tile tile = tile_at(index), next = tile;
+  if (walk.count > 0) {
+    int64_t index = 0;
+    Tile tile = tile_at(0), next = tile;
     clear();
     i32x8 fr[2], fc[2][FC];
     uint32_t xw[FR], ww[FC], xn[FR], wn[FC];  // scales of this and the next four steps
     bool more;
     int done = 0, at = 0;  // steps of the tile that are done; where the loads stand, in bytes along the contraction
     auto look_ahead = [&]() {
-      more = index + stride < end;
+      more = index + 1 < walk.count;
       if (more) {
-        next = tile_at(index + stride);
+        next = tile_at(index + 1);
         look_up(next);
       }
     };
@@ -593,7 +589,7 @@ __global__ __launch_bounds__(512) void e4m3_tile_kernel(E4m3Args a, int col_tile
         store(tile);
         if (!more) break;
         clear();
-        index += stride;
+        ++index;
         tile = next;
         begin_scales(tile);
         done = 0;

@@ -261,43 +261,36 @@ __global__ __launch_bounds__(WR * WC * 64) void grouped_tile_kernel(
     int64_t pbegin;
     int length;
   };
-  const TileList<BM> list(offsets, FORM == kGradient ? 0 : groups, rows);
-  int64_t index, end;  // tiles of this workgroup: index, index + stride ... below end
-  int stride;
-  if (FORM == kGradient) {  // every die has a part of every group, as groups may be of very different length
-    index = blockIdx.x;
-    end = (int64_t)groups * row_tiles * col_tiles;
-    stride = gridDim.x;
-  } else {
-    // an eighth of the tiles to the workgroups of each die, neighbouring tiles at one time
-    const int64_t total = (int64_t)list.total * col_tiles, share = (total + 7) / 8;
-    stride = gridDim.x >> 3;
-    index = (int64_t)(blockIdx.x & 7) * share + (blockIdx.x >> 3);
-    end = min(total, (int64_t)((blockIdx.x & 7) + 1) * share);
-  }
-  auto tile_at = [&](int64_t i) {
-    Tile t;
+  const TileWalk<BM> walk(offsets, FORM == kGradient ? 0 : groups, rows, FORM == kGradient ? 1 : col_tiles);
+  const GroupOrder by_length(offsets, FORM == kGradient ? groups : 0, rows);
+  const int per_group = row_tiles * col_tiles;  // gradient
+  // A gradient's tiles take as long as their groups are.  From the longest group to the shortest they are dealt out to all
+  // workgroups, to and fro.
+  const int64_t count =
+      FORM == kGradient ? ((int64_t)groups * per_group + gridDim.x - 1) / gridDim.x : walk.count;
+  auto tile_at = [&](int64_t i, Tile& t) {  // false: there is none (only the last one of a gradient)
     if (FORM == kGradient) {
-      t.group = (int)(i / (row_tiles * col_tiles));
-      const int in = (int)(i - (int64_t)t.group * (row_tiles * col_tiles));
+      const int64_t at = i * gridDim.x + (i & 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
+      if (at >= (int64_t)groups * per_group) return false;
+      const int g = (int)(at / per_group), in = (int)(at - (int64_t)g * per_group);
+      t.group = by_length.at(g);
       t.r0 = in / col_tiles * BM;
       t.c0 = in % col_tiles * BN;
       t.rn = min(BM, outr - t.r0);
-      const GroupRange g = group_range(offsets, groups, rows, t.group);
-      t.pbegin = g.begin;
-      t.length = (int)(g.end - g.begin);
+      const GroupRange r = group_range(offsets, groups, rows, t.group);
+      t.pbegin = r.begin;
+      t.length = (int)(r.end - r.begin);
     } else {
-      const int row_tile = (int)(i / col_tiles);
-      const RowTile r = list.at(row_tile);
+      const RowTile r = walk.at(i);
       t.group = r.group;
       t.r0 = 0;
       t.rn = r.count;
       t.pbegin = r.begin;
-      t.c0 = (int)(i - (int64_t)row_tile * col_tiles) * BN;
+      t.c0 = r.col * BN;
       t.length = depth;
     }
     t.cn = min(BN, outc - t.c0);
-    return t;
+    return true;
   };
 
   // ---- what a lane loads ----
@@ -437,8 +430,9 @@ __global__ __launch_bounds__(WR * WC * 64) void grouped_tile_kernel(
   constexpr int PAIRS = FR / 2, CL = LC / PAIRS;
   static_assert(CL * PAIRS == LC, "");
   constexpr int EARLY = PAIRS > 2 ? LR / PAIRS * (PAIRS - 2) : 0;  // loads of the rows' operand before the second meeting
-  if (index < end) {
-    Tile tile = tile_at(index), next = tile;
+  Tile tile, next;
+  int64_t index = 0;
+  if (count > 0 && tile_at(0, tile)) {
     clear();
     Chunk fr[2][2], fc[2][FC];
     constexpr int LEAST = FORM == kGradient ? 3 : 2;
@@ -492,11 +486,8 @@ __global__ __launch_bounds__(WR * WC * 64) void grouped_tile_kernel(
       look_further();
     };
     auto look_ahead = [&]() {
-      more = index + stride < end;
-      if (more) {
-        next = tile_at(index + stride);
-        look_up_rows(next);
-      }
+      more = index + 1 < count && tile_at(index + 1, next);
+      if (more) look_up_rows(next);
     };
     int cnow = 0, rnow = 1, cnext = 2, rnext = 3, ahead = 4;  // buffers of this step, of the next one, and the free one
     look_up_rows(tile);
@@ -568,7 +559,7 @@ __global__ __launch_bounds__(WR * WC * 64) void grouped_tile_kernel(
         store(tile);
         if (!more) break;
         clear();
-        index += stride;
+        ++index;
         tile = next;
         left = steps_of(tile);
         look_ahead();

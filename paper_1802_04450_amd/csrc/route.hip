@@ -14,16 +14,43 @@ constexpr float kNone = -INFINITY;
 // ---- the assignment ---------------------------------------------------------------------------------------------------
 // LANES lanes hold a row, lane l its scores l * VPL ... l * VPL + VPL - 1: of lanes that hold the same largest score the first
 // then holds the lowest index, and the loads are wide.
+// Within 16 lanes the values go round by lane rotations, across the four sixteens of a wave by way of scalar registers.
+template <int N>
+__device__ __forceinline__ float rotated(float v) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x120 + N, 0xf, 0xf, false));
+}
+__device__ __forceinline__ float of_lane(float v, int lane) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane)); }
 template <int LANES>
 __device__ __forceinline__ float group_max(float v) {
-#pragma unroll
-  for (int s = 1; s < LANES; s <<= 1) v = fmaxf(v, __shfl_xor(v, s));
+  v = fmaxf(v, rotated<8>(v));
+  v = fmaxf(v, rotated<4>(v));
+  v = fmaxf(v, rotated<2>(v));
+  v = fmaxf(v, rotated<1>(v));
+  if (LANES == 64) v = fmaxf(fmaxf(of_lane(v, 0), of_lane(v, 16)), fmaxf(of_lane(v, 32), of_lane(v, 48)));
+  return v;
+}
+template <int N>
+__device__ __forceinline__ uint32_t rotated(uint32_t v) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x120 + N, 0xf, 0xf, false);
+}
+template <int LANES>
+__device__ __forceinline__ uint32_t group_max(uint32_t v) {
+  v = max(v, rotated<8>(v));
+  v = max(v, rotated<4>(v));
+  v = max(v, rotated<2>(v));
+  v = max(v, rotated<1>(v));
+  if (LANES == 64)
+    v = max(max((uint32_t)__builtin_amdgcn_readlane(v, 0), (uint32_t)__builtin_amdgcn_readlane(v, 16)),
+            max((uint32_t)__builtin_amdgcn_readlane(v, 32), (uint32_t)__builtin_amdgcn_readlane(v, 48)));
   return v;
 }
 template <int LANES>
 __device__ __forceinline__ float group_sum(float v) {
-#pragma unroll
-  for (int s = 1; s < LANES; s <<= 1) v += __shfl_xor(v, s);
+  v += rotated<8>(v);
+  v += rotated<4>(v);
+  v += rotated<2>(v);
+  v += rotated<1>(v);
+  if (LANES == 64) v = (of_lane(v, 0) + of_lane(v, 16)) + (of_lane(v, 32) + of_lane(v, 48));
   return v;
 }
 
@@ -49,7 +76,7 @@ __device__ __forceinline__ void load_scores(const T* row, const uint8_t* allowed
         }
       }
 #pragma unroll
-      for (int u = 0; u < E; ++u) v[c + u] = v[c + u] > kNone ? v[c + u] : kNone;  // NaN too
+      for (int u = 0; u < E; ++u) v[c + u] = fmaxf(v[c + u], kNone);  // NaN too
     } else {
 #pragma unroll
       for (int u = 0; u < E; ++u) v[c + u] = kNone;
@@ -57,137 +84,281 @@ __device__ __forceinline__ void load_scores(const T* row, const uint8_t* allowed
   }
 }
 
+// exp(x) for the sum over all clusters: the rounding of x log2(e) is 2^-24 |x| of a term exp(x), 2^-25 of the sum at most.
+__device__ __forceinline__ float term(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504f); }
+
+// A 16-bit score and its cluster as one number: larger for a larger score, of equal scores (the zeros of both signs among them) for
+// the lower cluster, 0 for what is ruled out.
+template <typename T>
+__device__ __forceinline__ uint32_t key_of(float v, int c) {
+  const uint32_t bits = __builtin_bit_cast(uint16_t, static_cast<T>(v + 0.0f));
+  const uint32_t up = bits & 0x8000u ? bits ^ 0xffffu : bits ^ 0x8000u;
+  return v > kNone ? up << 16 | (uint32_t)(0xffff - c) : 0u;
+}
+template <typename T>
+__device__ __forceinline__ float score_of(uint32_t key) {
+  const uint32_t up = key >> 16;
+  return static_cast<float>(__builtin_bit_cast(T, (uint16_t)(up & 0x8000u ? up ^ 0x8000u : up ^ 0xffffu)));
+}
+
+// The choices of the row that LANES lanes hold: lane s < t gets the s-th in `at` (-1: none) and its weight.  Scores of 16 bits
+// take a third of the instructions (32,768 rows of 128, t = 8: 14 us with the way that 32 bits go).
+template <typename T, int LANES, int VPL>
+__device__ __forceinline__ void choose(float (&v)[VPL], int t, int normalize, int lane, int shift, int& at, float& weight) {
+  float top = 0.0f, total = 0.0f, mine = kNone;
+  at = -1;
+  auto after_first = [&](float m) {
+    top = m > kNone ? m : 0.0f;
+    if (!normalize) {
+      float sum = 0.0f;
+#pragma unroll
+      for (int c = 0; c < VPL; ++c) sum += term(v[c] - top);
+      total = group_sum<LANES>(sum);
+    }
+  };
+  if constexpr (sizeof(T) == 2) {
+    uint32_t key[VPL];
+#pragma unroll
+    for (int c = 0; c < VPL; ++c) key[c] = key_of<T>(v[c], lane * VPL + c);
+    for (int s = 0; s < t; ++s) {
+      uint32_t best = key[0];
+#pragma unroll
+      for (int c = 1; c < VPL; ++c) best = max(best, key[c]);
+      best = group_max<LANES>(best);
+      if (s == 0) after_first(best ? score_of<T>(best) : kNone);
+      if (lane == s && best) {
+        at = 0xffff - (int)(best & 0xffffu);
+        mine = score_of<T>(best);
+      }
+#pragma unroll
+      for (int c = 0; c < VPL; ++c) key[c] = key[c] == best ? 0u : key[c];
+    }
+  } else {
+    for (int s = 0; s < t; ++s) {
+      float best = v[0];
+      int c0 = 0;
+#pragma unroll
+      for (int c = 1; c < VPL; ++c) {
+        c0 = v[c] > best ? c : c0;
+        best = fmaxf(best, v[c]);
+      }
+      const float m = group_max<LANES>(best);
+      if (s == 0) after_first(m);
+      uint64_t who = __ballot(best == m && m > kNone) >> shift;
+      if constexpr (LANES < 64) who &= (1ull << LANES) - 1;
+      if (who != 0) {
+        const int owner = __ffsll((unsigned long long)who) - 1;
+        const int chosen = __shfl(c0, shift + owner) + owner * VPL;
+        const int out = lane == owner ? c0 : -1;
+#pragma unroll
+        for (int c = 0; c < VPL; ++c) v[c] = c == out ? kNone : v[c];
+        if (lane == s) {
+          at = chosen;
+          mine = m;
+        }
+      }
+    }
+  }
+  const float e = at >= 0 ? expf(mine - top) : 0.0f;
+  if (normalize) total = group_sum<16>(e);  // t <= 16; of a wave's four sixteens only the first holds choices, and only it goes on
+  weight = at >= 0 ? e / total : 0.0f;
+}
+
 // A workgroup takes `chunk` rows (a multiple of the rows that it holds at once) and leaves in hist[blockIdx.x * k + c] how many
-// of their choices are cluster c.
+// of their choices are cluster c.  The next row is on its way while one is looked through.
+constexpr int kRouteThreads = 512;
 template <typename T, int LANES, int VPL, bool WIDE>
-__global__ __launch_bounds__(kThreads) void route_kernel(const T* __restrict__ scores, int64_t ld,
+__global__ __launch_bounds__(kRouteThreads) void route_kernel(const T* __restrict__ scores, int64_t ld,
                                                          const uint8_t* __restrict__ allowed, int64_t lda, int64_t n, int k, int t,
                                                          int normalize, int chunk, int32_t* __restrict__ idx,
                                                          float* __restrict__ weight, int32_t* __restrict__ hist) {
   extern __shared__ int32_t count[];
-  for (int c = threadIdx.x; c < k; c += kThreads) count[c] = 0;
+  for (int c = threadIdx.x; c < k; c += kRouteThreads) count[c] = 0;
   __syncthreads();
-  constexpr int ROWS = kThreads / LANES;
+  constexpr int ROWS = kRouteThreads / LANES;
   const int lane = threadIdx.x & (LANES - 1);
   const int first = lane * VPL;
   const int shift = (threadIdx.x & (kWave - 1)) & ~(LANES - 1);
   const int64_t end = min(n, (int64_t)(blockIdx.x + 1) * chunk);
-  for (int64_t i = (int64_t)blockIdx.x * chunk + threadIdx.x / LANES; i < end; i += ROWS) {
+  const int64_t begin = (int64_t)blockIdx.x * chunk + threadIdx.x / LANES;
+  float next[VPL];
+  if (begin < end) load_scores<T, VPL, WIDE>(scores + begin * ld, allowed ? allowed + begin * lda : nullptr, first, k, next);
+  for (int64_t i = begin; i < end; i += ROWS) {
     float v[VPL];
-    load_scores<T, VPL, WIDE>(scores + i * ld, allowed ? allowed + i * lda : nullptr, first, k, v);
-    float top = 0.0f, total = 0.0f, mine = 0.0f;
-    int at = -1;
-    for (int s = 0; s < t; ++s) {
-      float best = v[0];
 #pragma unroll
-      for (int c = 1; c < VPL; ++c) best = fmaxf(best, v[c]);
-      const float m = group_max<LANES>(best);
-      if (s == 0) {
-        top = m > kNone ? m : 0.0f;
-        if (!normalize) {
-          float sum = 0.0f;
-#pragma unroll
-          for (int c = 0; c < VPL; ++c) sum += expf(v[c] - top);
-          total = group_sum<LANES>(sum);
-        }
-      }
-      uint64_t who = __ballot(best == m && m > kNone) >> shift;
-      if constexpr (LANES < 64) who &= (1ull << LANES) - 1;
-      const bool found = who != 0;
-      const int owner = found ? __ffsll((unsigned long long)who) - 1 : 0;
-      int c0 = 0;
-      if (found && lane == owner) {
-        bool hit = false;
-#pragma unroll
-        for (int c = 0; c < VPL; ++c) {
-          if (!hit && v[c] == m) {
-            hit = true;
-            c0 = c;
-            v[c] = kNone;
-          }
-        }
-        atomicAdd(&count[first + c0], 1);
-      }
-      const int chosen = __shfl(c0, shift + owner) + owner * VPL;
-      const float e = expf(m - top);
-      if (normalize && found) total += e;
-      if (lane == s && found) {
-        at = chosen;
-        mine = e;
-      }
-    }
+    for (int c = 0; c < VPL; ++c) v[c] = next[c];
+    if (i + ROWS < end)
+      load_scores<T, VPL, WIDE>(scores + (i + ROWS) * ld, allowed ? allowed + (i + ROWS) * lda : nullptr, first, k, next);
+    int at;
+    float w;
+    choose<T, LANES, VPL>(v, t, normalize, lane, shift, at, w);
     if (lane < t) {
       idx[i * t + lane] = at;
-      weight[i * t + lane] = at >= 0 ? mine / total : 0.0f;
+      weight[i * t + lane] = w;
+      if (at >= 0) atomicAdd(&count[at], 1);
     }
   }
   __syncthreads();
-  for (int c = threadIdx.x; c < k; c += kThreads) hist[(int64_t)blockIdx.x * k + c] = count[c];
+  for (int c = threadIdx.x; c < k; c += kRouteThreads) hist[(int64_t)blockIdx.x * k + c] = count[c];
 }
 
-// hist[b * k + c] becomes the number of choices of cluster c in the workgroups before b; totals[c] their number in all.
-__global__ __launch_bounds__(kThreads) void route_scan_kernel(int32_t* __restrict__ hist, int blocks, int k,
-                                                              int32_t* __restrict__ totals) {
-  const int c = blockIdx.x * kThreads + threadIdx.x;
-  if (c >= k) return;
-  int32_t sum = 0;
-  for (int b = 0; b < blocks; ++b) {
-    const int32_t h = hist[(int64_t)b * k + c];
-    hist[(int64_t)b * k + c] = sum;
-    sum += h;
+// The places of 64 slots, cluster c each (-1: none): what its cluster has taken so far (next[c], of this wave alone) plus the lanes
+// before it with the same cluster, found by one ballot for every bit of the cluster's number.
+__device__ __forceinline__ int32_t take_place(int32_t c, int bits, int lane, int32_t* next) {
+  uint64_t same = __ballot(c >= 0);
+  for (int b = 0; b < bits; ++b) {
+    const bool set = (c >> b) & 1;
+    const uint64_t m = __ballot(set);
+    same &= set ? m : ~m;
   }
-  totals[c] = sum;
+  int32_t p = -1;
+  if (c >= 0) {
+    p = next[c] + __popcll(same & ((1ull << lane) - 1));
+    if ((same >> lane) == 1ull) next[c] = p + 1;  // the last of them; every lane has read by then, a wave goes in step
+  }
+  return p;
+}
+__device__ __forceinline__ int bits_of(int k) { return k > 1 ? 32 - __builtin_clz(k - 1) : 0; }
+
+// Few slots: assignment and grouping in one workgroup.
+constexpr int kSmallThreads = 1024, kSmallSlots = 1024, kSmallClusters = 512;
+template <typename T, int LANES, int VPL, bool WIDE>
+__global__ __launch_bounds__(kSmallThreads) void route_small_kernel(const T* __restrict__ scores, int64_t ld,
+                                                                    const uint8_t* __restrict__ allowed, int64_t lda, int n, int k,
+                                                                    int t, int normalize, int32_t* __restrict__ idx,
+                                                                    float* __restrict__ weight, int32_t* __restrict__ offsets,
+                                                                    int32_t* __restrict__ order, int32_t* __restrict__ place) {
+  __shared__ int32_t count[kSmallClusters], slots[kSmallSlots];
+  for (int c = threadIdx.x; c < kSmallClusters; c += kSmallThreads) count[c] = 0;
+  __syncthreads();
+  const int lane = threadIdx.x & (LANES - 1);
+  const int shift = (threadIdx.x & (kWave - 1)) & ~(LANES - 1);
+  for (int i = threadIdx.x / LANES; i < n; i += kSmallThreads / LANES) {
+    float v[VPL];
+    load_scores<T, VPL, WIDE>(scores + i * ld, allowed ? allowed + i * lda : nullptr, lane * VPL, k, v);
+    int at;
+    float w;
+    choose<T, LANES, VPL>(v, t, normalize, lane, shift, at, w);
+    if (lane < t) {
+      idx[i * t + lane] = at;
+      weight[i * t + lane] = w;
+      slots[i * t + lane] = at;
+      if (at >= 0) atomicAdd(&count[at], 1);
+    }
+  }
+  __syncthreads();
+  if (threadIdx.x >= kWave) return;
+  const int l = threadIdx.x;
+  int32_t before = 0;
+  for (int c0 = 0; c0 < k; c0 += kWave) {
+    const int c = c0 + l;
+    const int32_t own = c < k ? count[c] : 0;
+    int32_t sum = own;
+#pragma unroll
+    for (int s = 1; s < kWave; s <<= 1) {
+      const int32_t o = __shfl_up(sum, s);
+      if (l >= s) sum += o;
+    }
+    if (c < k) {
+      count[c] = before + sum - own;
+      offsets[c] = before + sum - own;
+    }
+    before += __builtin_amdgcn_readlane(sum, kWave - 1);
+  }
+  if (l == 0) offsets[k] = before;
+  const int bits = bits_of(k);
+  for (int f0 = 0; f0 < n * t; f0 += kWave) {
+    const int f = f0 + l;
+    const int32_t p = take_place(f < n * t ? slots[f] : -1, bits, l, count);
+    if (f < n * t) {
+      place[f] = p;
+      if (p >= 0) order[p] = f;
+      if (f >= before) order[f] = -1;
+    }
+  }
 }
 
-// One wave a chunk puts the chunk's slots in their places, 64 at a time in slot order: a lane's place is what its cluster has
-// taken so far plus the lanes before it with the same cluster, found by one ballot for every bit of the cluster's number.
+// hist[b * k + c] becomes the number of choices of cluster c in the workgroups before b; totals[c] their number in all.  A workgroup
+// takes 8 clusters, 128 threads each a run of at most 8 workgroups: few enough for all loads to be under way at once (with runs
+// of 32 workgroups 9.2 us for 1,024 x 500 instead of 4.3).
+constexpr int kScanClusters = 8, kScanRuns = 128, kScanLength = 8;
+__global__ __launch_bounds__(kScanClusters* kScanRuns) void route_scan_kernel(int32_t* __restrict__ hist, int blocks, int k,
+                                                                            int32_t* __restrict__ totals) {
+  __shared__ int32_t sums[kScanRuns * kScanClusters / kWave][kScanClusters];
+  const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+  const int c = blockIdx.x * kScanClusters + threadIdx.x % kScanClusters;
+  const int length = (blocks + kScanRuns - 1) / kScanRuns;
+  const int b0 = threadIdx.x / kScanClusters * length;
+  int32_t h[kScanLength];
+#pragma unroll
+  for (int u = 0; u < kScanLength; ++u) h[u] = c < k && u < length && b0 + u < blocks ? hist[(int64_t)(b0 + u) * k + c] : 0;
+  int32_t own = 0;
+#pragma unroll
+  for (int u = 0; u < kScanLength; ++u) {
+    const int32_t v = h[u];
+    h[u] = own;
+    own += v;
+  }
+  int32_t sum = own;  // over the runs of the wave up to this one
+#pragma unroll
+  for (int s = kScanClusters; s < kWave; s <<= 1) {
+    const int32_t o = __shfl_up(sum, s);
+    if (lane >= s) sum += o;
+  }
+  if (lane >= kWave - kScanClusters) sums[wave][lane % kScanClusters] = sum;
+  __syncthreads();
+  int32_t before = sum - own;
+  for (int w = 0; w < wave; ++w) before += sums[w][lane % kScanClusters];
+  if (c >= k) return;
+#pragma unroll
+  for (int u = 0; u < kScanLength; ++u)
+    if (u < length && b0 + u < blocks) hist[(int64_t)(b0 + u) * k + c] = before + h[u];
+  if (threadIdx.x / kScanClusters == kScanRuns - 1) totals[c] = before + own;
+}
+
+// One wave a chunk puts the chunk's slots in their places, 64 at a time in slot order.
 __global__ __launch_bounds__(kWave) void route_place_kernel(const int32_t* __restrict__ idx, int64_t n, int k, int t, int chunk,
                                                             const int32_t* __restrict__ hist, const int32_t* __restrict__ totals,
                                                             int32_t* __restrict__ offsets, int32_t* __restrict__ order,
                                                             int32_t* __restrict__ place) {
   extern __shared__ int32_t next[];
   const int lane = threadIdx.x;
-  int32_t before = 0;
-  for (int c0 = 0; c0 < k; c0 += kWave) {  // exclusive sum of the totals
-    const int c = c0 + lane;
-    const int32_t own = c < k ? totals[c] : 0;
-    int32_t sum = own;
-#pragma unroll
-    for (int s = 1; s < kWave; s <<= 1) {
-      const int32_t o = __shfl_up(sum, s);
-      if (lane >= s) sum += o;
-    }
-    if (c < k) {
-      next[c] = before + sum - own + hist[(int64_t)blockIdx.x * k + c];
-      if (blockIdx.x == 0) offsets[c] = before + sum - own;
-    }
-    before += __shfl(sum, kWave - 1);
+  // exclusive sum of the totals: a lane adds up a run of clusters, then the lanes their sums
+  const int per = (k + kWave - 1) / kWave;
+  const int c0 = lane * per, c1 = min(c0 + per, k);
+  int32_t own = 0;
+  for (int c = c0; c < c1; ++c) {
+    next[c] = own;
+    own += totals[c];
   }
-  if (blockIdx.x == 0 && lane == 0) offsets[k] = before;
+  int32_t sum = own;
+#pragma unroll
+  for (int s = 1; s < kWave; s <<= 1) {
+    const int32_t o = __shfl_up(sum, s);
+    if (lane >= s) sum += o;
+  }
+  const int32_t all = __builtin_amdgcn_readlane(sum, kWave - 1);
+  for (int c = c0; c < c1; ++c) next[c] += sum - own;
   __syncthreads();
-  int bits = 0;
-  while ((1 << bits) < k) ++bits;
+  for (int c = lane; c < k; c += kWave) {
+    if (blockIdx.x == 0) offsets[c] = next[c];
+    next[c] += hist[(int64_t)blockIdx.x * k + c];
+  }
+  if (blockIdx.x == 0 && lane == 0) offsets[k] = all;
+  __syncthreads();
+  const int bits = bits_of(k);
   const int64_t begin = (int64_t)blockIdx.x * chunk * t, end = min(n, (int64_t)(blockIdx.x + 1) * chunk) * t;
+  int32_t ahead = begin + lane < end ? idx[begin + lane] : -1;
   for (int64_t f0 = begin; f0 < end; f0 += kWave) {
     const int64_t f = f0 + lane;
-    const int32_t c = f < end ? idx[f] : -1;
-    uint64_t same = __ballot(c >= 0);
-    for (int b = 0; b < bits; ++b) {
-      const bool set = (c >> b) & 1;
-      const uint64_t m = __ballot(set);
-      same &= set ? m : ~m;
-    }
-    if (c >= 0) {
-      const int rank = __popcll(same & ((1ull << lane) - 1));
-      const int32_t p = next[c] + rank;
+    const int32_t c = ahead;
+    ahead = f + kWave < end ? idx[f + kWave] : -1;
+    const int32_t p = take_place(c, bits, lane, next);
+    if (f < end) {
       place[f] = p;
-      order[p] = (int32_t)f;
-      if ((same >> lane) == 1ull) next[c] = p + 1;  // the last of them; after every lane has read, in program order
-    } else if (f < end) {
-      place[f] = -1;
+      if (p >= 0) order[p] = (int32_t)f;
+      if (f >= all) order[f] = -1;
     }
-    if (f < end && f >= before) order[f] = -1;
-    __syncthreads();
   }
 }
 
@@ -195,41 +366,66 @@ int route_chunk(int64_t n, int k) {
   // At most 1,024 workgroups, and counters of at most 2^20 words for all of them: the scan reads them all.
   int64_t blocks = (int64_t)(1 << 20) / k;
   if (blocks > 1024) blocks = 1024;
-  if (blocks < 1) blocks = 1;
   const int64_t rows = (n + blocks - 1) / blocks;
   return (int)((rows + 15) / 16 * 16);
 }
 int route_blocks(int64_t n, int k) { return (int)((n + route_chunk(n, k) - 1) / route_chunk(n, k)); }
+// One launch instead of three where a workgroup's 16 waves have little to do.
+bool route_small(int64_t n, int k, int t) { return n * t <= kSmallSlots && k <= kSmallClusters; }
+
+struct RouteOut {
+  int32_t* idx;
+  float* weight;
+  int32_t *offsets, *order, *place, *hist;
+};
 
 template <typename T, int LANES, int VPL>
 hipError_t route_typed(const T* scores, int64_t ld, const uint8_t* allowed, int64_t lda, int64_t n, int k, int t, bool normalize,
-                       int32_t* idx, float* weight, int32_t* hist, hipStream_t st) {
+                       const RouteOut& o, hipStream_t st) {
   constexpr int E = VPL * (int)sizeof(T) < 16 ? VPL : 16 / (int)sizeof(T);
   const bool wide = k % E == 0 && ld % E == 0 && reinterpret_cast<uintptr_t>(scores) % (E * sizeof(T)) == 0 &&
                     (!allowed || (lda % E == 0 && reinterpret_cast<uintptr_t>(allowed) % E == 0));
+  if constexpr (LANES * VPL <= kSmallClusters) {
+    if (route_small(n, k, t)) {
+      if (wide)
+        route_small_kernel<T, LANES, VPL, true><<<1, kSmallThreads, 0, st>>>(scores, ld, allowed, lda, (int)n, k, t, normalize, o.idx,
+                                                                            o.weight, o.offsets, o.order, o.place);
+      else
+        route_small_kernel<T, LANES, VPL, false><<<1, kSmallThreads, 0, st>>>(scores, ld, allowed, lda, (int)n, k, t, normalize, o.idx,
+                                                                             o.weight, o.offsets, o.order, o.place);
+      return hipGetLastError();
+    }
+  }
   const int chunk = route_chunk(n, k), blocks = route_blocks(n, k);
   const size_t lds = sizeof(int32_t) * k;
   if (wide)
-    route_kernel<T, LANES, VPL, true><<<blocks, kThreads, lds, st>>>(scores, ld, allowed, lda, n, k, t, normalize, chunk, idx,
-                                                                    weight, hist);
+    route_kernel<T, LANES, VPL, true><<<blocks, kRouteThreads, lds, st>>>(scores, ld, allowed, lda, n, k, t, normalize, chunk, o.idx,
+                                                                    o.weight, o.hist);
   else
-    route_kernel<T, LANES, VPL, false><<<blocks, kThreads, lds, st>>>(scores, ld, allowed, lda, n, k, t, normalize, chunk, idx,
-                                                                     weight, hist);
+    route_kernel<T, LANES, VPL, false><<<blocks, kRouteThreads, lds, st>>>(scores, ld, allowed, lda, n, k, t, normalize, chunk, o.idx,
+                                                                     o.weight, o.hist);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  int32_t* totals = o.hist + (size_t)blocks * k;
+  route_scan_kernel<<<(k + kScanClusters - 1) / kScanClusters, kScanClusters * kScanRuns, 0, st>>>(o.hist, blocks, k, totals);
+  e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  route_place_kernel<<<blocks, kWave, lds, st>>>(o.idx, n, k, t, chunk, o.hist, totals, o.offsets, o.order, o.place);
   return hipGetLastError();
 }
 
 template <typename T>
-hipError_t route_sized(const T* s, int64_t ld, const uint8_t* a, int64_t lda, int64_t n, int k, int t, bool norm, int32_t* idx,
-                       float* w, int32_t* hist, hipStream_t st) {
-  if (k <= 16) return route_typed<T, 16, 1>(s, ld, a, lda, n, k, t, norm, idx, w, hist, st);
-  if (k <= 32) return route_typed<T, 16, 2>(s, ld, a, lda, n, k, t, norm, idx, w, hist, st);
-  if (k <= 64) return route_typed<T, 16, 4>(s, ld, a, lda, n, k, t, norm, idx, w, hist, st);
-  if (k <= 128) return route_typed<T, 16, 8>(s, ld, a, lda, n, k, t, norm, idx, w, hist, st);
-  if (k <= 256) return route_typed<T, 64, 4>(s, ld, a, lda, n, k, t, norm, idx, w, hist, st);
-  if (k <= 512) return route_typed<T, 64, 8>(s, ld, a, lda, n, k, t, norm, idx, w, hist, st);
-  if (k <= 1024) return route_typed<T, 64, 16>(s, ld, a, lda, n, k, t, norm, idx, w, hist, st);
-  if (k <= 2048) return route_typed<T, 64, 32>(s, ld, a, lda, n, k, t, norm, idx, w, hist, st);
-  return route_typed<T, 64, 64>(s, ld, a, lda, n, k, t, norm, idx, w, hist, st);
+hipError_t route_sized(const T* s, int64_t ld, const uint8_t* a, int64_t lda, int64_t n, int k, int t, bool norm, const RouteOut& o,
+                       hipStream_t st) {
+  if (k <= 16) return route_typed<T, 16, 1>(s, ld, a, lda, n, k, t, norm, o, st);
+  if (k <= 32) return route_typed<T, 16, 2>(s, ld, a, lda, n, k, t, norm, o, st);
+  if (k <= 64) return route_typed<T, 16, 4>(s, ld, a, lda, n, k, t, norm, o, st);
+  if (k <= 128) return route_typed<T, 16, 8>(s, ld, a, lda, n, k, t, norm, o, st);
+  if (k <= 256) return route_typed<T, 64, 4>(s, ld, a, lda, n, k, t, norm, o, st);
+  if (k <= 512) return route_typed<T, 64, 8>(s, ld, a, lda, n, k, t, norm, o, st);
+  if (k <= 1024) return route_typed<T, 64, 16>(s, ld, a, lda, n, k, t, norm, o, st);
+  if (k <= 2048) return route_typed<T, 64, 32>(s, ld, a, lda, n, k, t, norm, o, st);
+  return route_typed<T, 64, 64>(s, ld, a, lda, n, k, t, norm, o, st);
 }
 
 // ---- gradient of the scores ---------------------------------------------------------------------------------------------
@@ -395,29 +591,31 @@ __global__ __launch_bounds__(kThreads) void combine_kernel(const T* __restrict__
   store_part<T, E>(out + i * ldo + j, sum);
 }
 
-// One workgroup a row: dz_p = w dout_i and dw = <dout_i, z_p> for its t places, and zeros into rows of dz where nothing has its
-// place.
+// One wave a slot: dz_p = w dout_i and dw = <dout_i, z_p> for its place p; and zeros into grouped row q, the wave's number, where
+// nothing has its place.  A row's slots are neighbours, so that dout_i comes out of L1 or L2 for all but the first (32,768 rows, 4
+// slots, 1,024 values of 16 bits: 603 MB in 161 us with a workgroup a row).
 template <typename T, int E>
 __global__ __launch_bounds__(kThreads) void combine_backward_kernel(const T* __restrict__ dout, int64_t ldo, const T* __restrict__ z,
                                                                     int64_t ldz, int64_t rows, const int32_t* __restrict__ place,
                                                                     const float* __restrict__ weight,
-                                                                    const int32_t* __restrict__ order, int64_t n, int t, int d,
+                                                                    const int32_t* __restrict__ order, int64_t slots, int t, int d,
                                                                     T* __restrict__ dz, int64_t lddz, float* __restrict__ dweight) {
-  __shared__ float part[kThreads / kWave];
-  const int64_t i = blockIdx.x;
-  for (int s = 0; s < t && i < n; ++s) {
-    const int32_t p = place[i * t + s];
+  const int64_t q = (int64_t)blockIdx.x * (kThreads / kWave) + threadIdx.x / kWave;
+  const int lane = threadIdx.x & (kWave - 1);
+  if (q < slots) {
+    const int32_t p = place[q];
     float dot = 0.0f;
     if (p >= 0 && p < rows) {
-      const float w = weight ? weight[i * t + s] : 1.0f;
-      for (int j = threadIdx.x * E; j < d; j += kThreads * E) {
+      const float w = weight ? weight[q] : 1.0f;
+      const T* g0 = dout + (uint32_t)q / (uint32_t)t * ldo;
+      for (int j = lane * E; j < d; j += kWave * E) {
         float g[E], v[E], o[E];
-        load_part<T, E>(dout + i * ldo + j, g);
+        load_part<T, E>(g0 + j, g);
+        if (dweight) load_part<T, E>(z + p * ldz + j, v);
 #pragma unroll
         for (int u = 0; u < E; ++u) o[u] = w * g[u];
         store_part<T, E>(dz + p * lddz + j, o);
         if (dweight) {
-          load_part<T, E>(z + p * ldz + j, v);
 #pragma unroll
           for (int u = 0; u < E; ++u) dot += g[u] * v[u];
         }
@@ -425,22 +623,14 @@ __global__ __launch_bounds__(kThreads) void combine_backward_kernel(const T* __r
     }
     if (dweight) {
       dot = group_sum<kWave>(dot);
-      if ((threadIdx.x & (kWave - 1)) == 0) part[threadIdx.x / kWave] = dot;
-      __syncthreads();
-      if (threadIdx.x == 0) {
-        float sum = 0.0f;
-        for (int q = 0; q < kThreads / kWave; ++q) sum += part[q];
-        dweight[i * t + s] = sum;
-      }
-      __syncthreads();
+      if (lane == 0) dweight[q] = dot;
     }
   }
-  for (int64_t p = i; p < rows; p += gridDim.x) {
-    if (order[p] >= 0) continue;
+  if (q < rows && order[q] < 0) {
     float o[E];
 #pragma unroll
     for (int u = 0; u < E; ++u) o[u] = 0.0f;
-    for (int j = threadIdx.x * E; j < d; j += kThreads * E) store_part<T, E>(dz + p * lddz + j, o);
+    for (int j = lane * E; j < d; j += kWave * E) store_part<T, E>(dz + q * lddz + j, o);
   }
 }
 
@@ -468,14 +658,15 @@ hipError_t combine_backward_typed(const T* dout, int64_t ldo, const T* z, int64_
                                   const float* weight, const int32_t* order, int64_t n, int t, int d, T* dz, int64_t lddz,
                                   float* dweight, hipStream_t st) {
   constexpr int E = 16 / (int)sizeof(T);
-  const uint32_t blocks = (uint32_t)(n > 0 ? n : 1);
+  const int64_t slots = n * t, waves = slots > rows ? slots : rows;
+  const uint32_t blocks = (uint32_t)((waves + kThreads / kWave - 1) / (kThreads / kWave));
   const bool wide = d % E == 0 && wide_rows<T>(dout, ldo) && wide_rows<T>(dz, lddz) && (!dweight || wide_rows<T>(z, ldz));
   if (wide)
-    combine_backward_kernel<T, E><<<blocks, kThreads, 0, st>>>(dout, ldo, z, ldz, rows, place, weight, order, n, t, d, dz, lddz,
-                                                               dweight);
+    combine_backward_kernel<T, E><<<blocks, kThreads, 0, st>>>(dout, ldo, z, ldz, rows, place, weight, order, slots, t, d, dz,
+                                                               lddz, dweight);
   else
-    combine_backward_kernel<T, 1><<<blocks, kThreads, 0, st>>>(dout, ldo, z, ldz, rows, place, weight, order, n, t, d, dz, lddz,
-                                                               dweight);
+    combine_backward_kernel<T, 1><<<blocks, kThreads, 0, st>>>(dout, ldo, z, ldz, rows, place, weight, order, slots, t, d, dz,
+                                                               lddz, dweight);
   return hipGetLastError();
 }
 
@@ -498,22 +689,10 @@ hipError_t launch_route(const void* scores, int dtype, int64_t ld, const uint8_t
     zero_words_kernel<<<1, kThreads, 0, st>>>(offsets, k + 1);
     return hipGetLastError();
   }
-  const int blocks = route_blocks(n, k), chunk = route_chunk(n, k);
-  int32_t* hist = static_cast<int32_t*>(work);
-  int32_t* totals = hist + (size_t)blocks * k;
-  hipError_t e;
-  if (dtype == kF32)
-    e = route_sized(static_cast<const float*>(scores), ld, allowed, lda, n, k, t, normalize, idx, weight, hist, st);
-  else if (dtype == kBF16)
-    e = route_sized(static_cast<const __bf16*>(scores), ld, allowed, lda, n, k, t, normalize, idx, weight, hist, st);
-  else
-    e = route_sized(static_cast<const _Float16*>(scores), ld, allowed, lda, n, k, t, normalize, idx, weight, hist, st);
-  if (e != hipSuccess) return e;
-  route_scan_kernel<<<(k + kThreads - 1) / kThreads, kThreads, 0, st>>>(hist, blocks, k, totals);
-  e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  route_place_kernel<<<blocks, kWave, sizeof(int32_t) * k, st>>>(idx, n, k, t, chunk, hist, totals, offsets, order, place);
-  return hipGetLastError();
+  const RouteOut o{idx, weight, offsets, order, place, static_cast<int32_t*>(work)};
+  if (dtype == kF32) return route_sized(static_cast<const float*>(scores), ld, allowed, lda, n, k, t, normalize, o, st);
+  if (dtype == kBF16) return route_sized(static_cast<const __bf16*>(scores), ld, allowed, lda, n, k, t, normalize, o, st);
+  return route_sized(static_cast<const _Float16*>(scores), ld, allowed, lda, n, k, t, normalize, o, st);
 }
 
 hipError_t launch_route_backward(const void* scores, int dtype, int64_t ld, const uint8_t* allowed, int64_t lda, int64_t n,
