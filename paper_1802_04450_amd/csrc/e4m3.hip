@@ -337,6 +337,134 @@ __global__ __launch_bounds__(256) void e4m3_wide_kernel(E4m3Args a, int cols) {
   }
 }
 
+// ---- product, few rows a group -----------------------------------------------------------------------------------------------
+// As in 16 bits: every matrix that is met goes once from memory into the registers of the wave that needs it.  A wave has 16
+// columns and RF * 16 rows; KS of a workgroup's four waves share the columns, each with every KS-th run of two blocks of the
+// contraction, and their sums are added in order.  Results of 32 bits take the numbers as bf16 (see above).
+constexpr int kThinRun = 2;
+
+template <typename T, int RF, int KS>
+__global__ __launch_bounds__(256) void e4m3_thin_kernel(E4m3Args a, int col_tiles, int whole_stores) {
+  constexpr int CT = 4 / KS;
+  constexpr bool WIDE = sizeof(T) == 4;
+  __shared__ f32x4 part[KS > 1 ? (KS - 1) * CT * RF * 64 : 1];
+  const RowTile t = find_tile<RF * 16>(a.offsets, a.groups, a.rows, col_tiles);
+  if (t.group < 0) return;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int ks = wave % KS, ct = wave / KS;
+  const int c0 = (t.col * CT + ct) * 16;
+  const int sub = lane & 15, quad = lane >> 4;
+  const int steps = t.group == a.groups ? 0 : a.Kp / kScaleBlock;
+  f32x4 acc[RF];
+#pragma unroll
+  for (int r = 0; r < RF; ++r) acc[r] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  if (steps > 0 && c0 < a.N) {
+    const int col = min(c0 + sub, a.N - 1);
+    const uint8_t* w = a.w + (int64_t)t.group * a.ldg + (int64_t)col * a.ldw + quad * 32;
+    const uint8_t* ws = a.ws + (int64_t)t.group * a.ldgs + (int64_t)col * a.ldws;
+    const uint8_t *x[RF], *xs[RF];
+#pragma unroll
+    for (int r = 0; r < RF; ++r) {
+      const int row = r * 16 + sub;
+      const int64_t src = row < t.count ? source_row(a.order, t.begin + row, a.slots, a.xrows) : -1;
+      x[r] = src < 0 ? nullptr : a.x + src * a.ldx + quad * 32;
+      xs[r] = src < 0 ? nullptr : a.xs + src * a.ldxs;
+    }
+    i32x4 next[kThinRun][2];
+    int sn[kThinRun];
+    auto load = [&](int b) {
+#pragma unroll
+      for (int u = 0; u < kThinRun; ++u) {
+        const int at = min(b + u, steps - 1);  // a block that is not there is not used
+        next[u][0] = *reinterpret_cast<const i32x4*>(w + at * kScaleBlock);
+        next[u][1] = *reinterpret_cast<const i32x4*>(w + at * kScaleBlock + 16);
+        sn[u] = ws[at];
+      }
+    };
+    int b = ks * kThinRun;
+    load(min(b, steps - 1));
+    for (; b < steps; b += KS * kThinRun) {
+      i32x4 now[kThinRun][2];
+      int sw[kThinRun];
+#pragma unroll
+      for (int u = 0; u < kThinRun; ++u) {
+        now[u][0] = next[u][0];
+        now[u][1] = next[u][1];
+        sw[u] = sn[u];
+      }
+      if (b + KS * kThinRun < steps) load(b + KS * kThinRun);
+#pragma unroll
+      for (int r = 0; r < RF; ++r) {
+        if (r * 16 >= t.count) continue;
+        i32x4 f[kThinRun][2];
+        int sx[kThinRun];
+#pragma unroll
+        for (int u = 0; u < kThinRun; ++u) {
+          f[u][0] = f[u][1] = i32x4{0, 0, 0, 0};
+          sx[u] = 127;
+          if (x[r] && b + u < steps) {
+            f[u][0] = *reinterpret_cast<const i32x4*>(x[r] + (b + u) * kScaleBlock);
+            f[u][1] = *reinterpret_cast<const i32x4*>(x[r] + (b + u) * kScaleBlock + 16);
+            sx[u] = xs[r][b + u];
+          }
+        }
+#pragma unroll
+        for (int u = 0; u < kThinRun; ++u) {
+          if (b + u >= steps) break;
+          if constexpr (!WIDE) {
+            const i32x8 p = __builtin_shufflevector(now[u][0], now[u][1], 0, 1, 2, 3, 4, 5, 6, 7);
+            const i32x8 q = __builtin_shufflevector(f[u][0], f[u][1], 0, 1, 2, 3, 4, 5, 6, 7);
+            acc[r] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(p, q, acc[r], 0, 0, 0, sw[u], 0, sx[u]);
+          } else {
+            f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+              for (int e = 0; e < 4; e += 2)
+                sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen(now[u][h][e], now[u][h][e + 1]), widen(f[u][h][e], f[u][h][e + 1]),
+                                                              sum, 0, 0, 0);
+            // the lane's four results are of columns 4 quad ... 4 quad + 3, whose powers of two lie in those lanes
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int s = __shfl(sw[u], quad * 4 + i);
+              acc[r][i] += s == 255 || sx[u] == 255 ? NAN : ldexpf(sum[i], s + sx[u] - 254);
+            }
+          }
+        }
+      }
+    }
+  }
+  if (KS > 1) {
+    if (ks > 0) {
+#pragma unroll
+      for (int r = 0; r < RF; ++r) part[(((ks - 1) * CT + ct) * RF + r) * 64 + lane] = acc[r];
+    }
+    __syncthreads();
+    if (ks > 0) return;
+#pragma unroll
+    for (int q = 0; q < KS - 1; ++q)
+#pragma unroll
+      for (int r = 0; r < RF; ++r) acc[r] += part[((q * CT + ct) * RF + r) * 64 + lane];
+  }
+  typedef T Quad __attribute__((ext_vector_type(4)));
+#pragma unroll
+  for (int r = 0; r < RF; ++r) {
+    const int row = r * 16 + sub, col = c0 + quad * 4;
+    if (row >= t.count || col >= a.N) continue;
+    T* out = static_cast<T*>(a.y) + (t.begin + row) * a.ldy + col;
+    Quad q;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) q[u] = static_cast<T>(acc[r][u]);
+    if (whole_stores) {
+      *reinterpret_cast<Quad*>(out) = q;
+    } else {
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        if (col + u < a.N) out[u] = q[u];
+    }
+  }
+}
+
 // ---- product, 256 x 256 ---------------------------------------------------------------------------------------------------
 // Eight waves, 128 x 64 of the tile each.  A step is one block of the contraction, 128 bytes of every row; it goes through LDS as the
 // 16-bit products' steps do (five buffers that hold a step of one operand, pieces straight from memory, the columns' operand two
@@ -639,14 +767,43 @@ hipError_t dequantize_typed(const uint8_t* q, int64_t ldq, const uint8_t* scale,
   return hipGetLastError();
 }
 
+template <typename T, int RF>
+hipError_t thin_typed(const E4m3Args& a, hipStream_t st) {
+  const int tiles = (a.N + 15) / 16;
+  const int64_t met = a.rows < a.groups ? a.rows : a.groups;  // groups with rows, at most
+  // about 2,048 waves at work
+  const int ks = met * tiles >= 2048 ? 1 : met * tiles >= 1024 ? 2 : 4;
+  const int cols = (tiles + 4 / ks - 1) / (4 / ks);
+  const int64_t blocks = tile_bound(a.rows, a.groups, RF * 16, cols);
+  if (blocks > 0x7fffffff) return hipErrorInvalidConfiguration;
+  const int whole = a.N % 4 == 0 && a.ldy % 4 == 0 && reinterpret_cast<uintptr_t>(a.y) % (4 * sizeof(T)) == 0;
+  if (ks == 1)
+    e4m3_thin_kernel<T, RF, 1><<<(uint32_t)blocks, 256, 0, st>>>(a, cols, whole);
+  else if (ks == 2)
+    e4m3_thin_kernel<T, RF, 2><<<(uint32_t)blocks, 256, 0, st>>>(a, cols, whole);
+  else
+    e4m3_thin_kernel<T, RF, 4><<<(uint32_t)blocks, 256, 0, st>>>(a, cols, whole);
+  return hipGetLastError();
+}
+
 template <typename T>
 hipError_t product_typed(const E4m3Args& a, hipStream_t st) {
   const int cols = (a.N + kTile - 1) / kTile;
   const int64_t blocks = tile_bound(a.rows, a.groups, kTile, cols);
   if (blocks > 0x7fffffff) return hipErrorInvalidConfiguration;
+  // 256 x 256 tiles: results of 16 bits, two steps at least, offsets of 32 bits.
+  const bool tiled = sizeof(T) == 2 && a.Kp >= 2 * kScaleBlock && a.xrows * a.ldx < (int64_t)1 << 32 && a.N * a.ldw < (int64_t)1 << 32;
+  // Up to 4 rows a group the matrices are what takes time, and the kernel for few rows reads them as fast as any (64 groups of
+  // 1024 x 2048, 64 rows 23 us, tiles 28; 256 rows 31 and 31).  Beyond, tiles read them less often (1,024 rows 46 and 32), but where
+  // there are few of them a good part of the chip has nothing to do (256 rows, 4 groups of 2048 x 2048 22 us, tiles 26; 8 rows 13
+  // and 25).
+  const int side = tiled ? 256 : kTile;
+  const int64_t row_tiles = a.rows / side + a.groups, tiles = (row_tiles < a.rows ? row_tiles : a.rows) * ((a.N + side - 1) / side);
+  if (a.rows <= (int64_t)4 * a.groups) return thin_typed<T, 1>(a, st);
+  if (tiles < (tiled ? 128 : 512) && a.rows <= (int64_t)64 * a.groups)
+    return a.rows <= (int64_t)24 * a.groups ? thin_typed<T, 2>(a, st) : thin_typed<T, 4>(a, st);
   if constexpr (sizeof(T) == 2) {
-    // two steps at least, and offsets of 32 bits
-    if (a.Kp >= 2 * kScaleBlock && a.xrows * a.ldx < (int64_t)1 << 32 && a.N * a.ldw < (int64_t)1 << 32) {
+    if (tiled) {
       const int wcols = (a.N + 255) / 256;
       const int64_t n = tile_bound(a.rows, a.groups, 256, wcols);
       const int whole = a.N % 8 == 0 && a.ldy % 8 == 0 && reinterpret_cast<uintptr_t>(a.y) % 16 == 0;

@@ -182,6 +182,109 @@ __global__ __launch_bounds__(256) void grouped_any_kernel(const T* __restrict__ 
   }
 }
 
+// ---- few rows a group ----------------------------------------------------------------------------------------------------------
+// Every matrix that is met is read once, from memory straight into the registers of the wave that needs it, and that is what
+// bounds it.  A wave has 16 columns and RF * 16 rows; KS of a workgroup's four waves share the columns, each with every KS-th
+// run of RUN chunks of the contraction, and their sums are added in order at the end: as few columns as there are, enough
+// waves are at work.  A run of the matrix is on its way while one is used.  Rows of any alignment: a lane's 16 bytes may begin anywhere.
+constexpr int kThinRun = 4;
+
+template <typename T>
+__device__ __forceinline__ typename Matrix<T>::Chunk load_any(const T* p, int64_t left) {
+  typedef typename Matrix<T>::Chunk Chunk;
+  constexpr int CH = Matrix<T>::kChunk;
+  Chunk v;
+  if (left >= CH) {
+    __builtin_memcpy(&v, p, sizeof(v));
+  } else {
+#pragma unroll
+    for (int u = 0; u < CH; ++u) v[u] = u < left ? p[u] : static_cast<T>(0.0f);
+  }
+  return v;
+}
+
+template <typename T, int RF, int KS>
+__global__ __launch_bounds__(256) void grouped_thin_kernel(GroupedArgs a, int col_tiles, int whole_stores) {
+  typedef typename Matrix<T>::Chunk Chunk;
+  constexpr int CH = Matrix<T>::kChunk, CT = 4 / KS, BK = 4 * CH;
+  __shared__ f32x4 part[KS > 1 ? (KS - 1) * CT * RF * 64 : 1];
+  const RowTile t = find_tile<RF * 16>(a.offsets, a.groups, a.rows, col_tiles);
+  if (t.group < 0) return;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int ks = wave % KS, ct = wave / KS;
+  const int c0 = (t.col * CT + ct) * 16;
+  const int sub = lane & 15, quad = lane >> 4;
+  const int64_t K = t.group == a.groups ? 0 : a.K;
+  f32x4 acc[RF];
+#pragma unroll
+  for (int r = 0; r < RF; ++r) acc[r] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  if (K > 0 && c0 < a.N) {
+    const T* w = static_cast<const T*>(a.w) + (int64_t)t.group * a.ldg + (int64_t)min(c0 + sub, a.N - 1) * a.ldw + quad * CH;
+    const T* x[RF];
+#pragma unroll
+    for (int r = 0; r < RF; ++r) {
+      const int row = r * 16 + sub;
+      const int64_t src = row < t.count ? source_row(a.order, t.begin + row, a.slots, a.xrows) : -1;
+      x[r] = src < 0 ? nullptr : static_cast<const T*>(a.x) + src * a.ldx + quad * CH;
+    }
+    const int64_t step = (int64_t)KS * kThinRun * BK;
+    Chunk next[kThinRun];
+    int64_t e0 = (int64_t)ks * kThinRun * BK;
+#pragma unroll
+    for (int u = 0; u < kThinRun; ++u) next[u] = load_any<T>(w + e0 + u * BK, K - (e0 + u * BK + quad * CH));
+    for (; e0 < K; e0 += step) {
+      Chunk now[kThinRun];
+#pragma unroll
+      for (int u = 0; u < kThinRun; ++u) now[u] = next[u];
+      const int64_t e1 = e0 + step;
+      if (e1 < K) {
+#pragma unroll
+        for (int u = 0; u < kThinRun; ++u) next[u] = load_any<T>(w + e1 + u * BK, K - (e1 + u * BK + quad * CH));
+      }
+#pragma unroll
+      for (int r = 0; r < RF; ++r) {
+        if (r * 16 < t.count) {
+          Chunk f[kThinRun];
+#pragma unroll
+          for (int u = 0; u < kThinRun; ++u)
+            f[u] = load_any<T>(x[r] + e0 + u * BK, x[r] ? K - (e0 + u * BK + quad * CH) : 0);
+#pragma unroll
+          for (int u = 0; u < kThinRun; ++u) acc[r] = Matrix<T>::mma(now[u], f[u], acc[r]);
+        }
+      }
+    }
+  }
+  if (KS > 1) {
+    if (ks > 0) {
+#pragma unroll
+      for (int r = 0; r < RF; ++r) part[(((ks - 1) * CT + ct) * RF + r) * 64 + lane] = acc[r];
+    }
+    __syncthreads();
+    if (ks > 0) return;
+#pragma unroll
+    for (int q = 0; q < KS - 1; ++q)
+#pragma unroll
+      for (int r = 0; r < RF; ++r) acc[r] += part[((q * CT + ct) * RF + r) * 64 + lane];
+  }
+  typedef T Quad __attribute__((ext_vector_type(4)));
+#pragma unroll
+  for (int r = 0; r < RF; ++r) {
+    const int row = r * 16 + sub, col = c0 + quad * 4;
+    if (row >= t.count || col >= a.N) continue;
+    T* out = static_cast<T*>(a.y) + (t.begin + row) * a.ldy + col;
+    Quad q;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) q[u] = static_cast<T>(acc[r][u]);
+    if (whole_stores) {
+      *reinterpret_cast<Quad*>(out) = q;
+    } else {
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        if (col + u < a.N) out[u] = q[u];
+    }
+  }
+}
+
 // ---- whole 16-byte pieces, 16-bit types --------------------------------------------------------------------------------------
 // A BM x BN tile by WR x WC waves.  The contraction goes through LDS in steps of 64, in five buffers that hold a step of one
 // operand each: while two are read, three are filled, the columns' operand two steps ahead and the rows' one and a half.  Pieces go
@@ -586,6 +689,25 @@ bool whole_chunks(const void* p, int64_t ld) {
   return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % Matrix<T>::kChunk == 0;
 }
 
+template <typename T, int RF>
+hipError_t thin_typed(const GroupedArgs& a, hipStream_t st) {
+  const int tiles = (a.N + 15) / 16;
+  const int64_t met = a.rows < a.groups ? a.rows : a.groups;  // groups with rows, at most
+  // about 2,048 waves at work
+  const int ks = met * tiles >= 2048 ? 1 : met * tiles >= 1024 ? 2 : 4;
+  const int cols = (tiles + 4 / ks - 1) / (4 / ks);
+  const int64_t blocks = tile_bound(a.rows, a.groups, RF * 16, cols);
+  if (blocks > 0x7fffffff) return hipErrorInvalidConfiguration;
+  const int whole = a.N % 4 == 0 && a.ldy % 4 == 0 && reinterpret_cast<uintptr_t>(a.y) % (4 * sizeof(T)) == 0;
+  if (ks == 1)
+    grouped_thin_kernel<T, RF, 1><<<(uint32_t)blocks, 256, 0, st>>>(a, cols, whole);
+  else if (ks == 2)
+    grouped_thin_kernel<T, RF, 2><<<(uint32_t)blocks, 256, 0, st>>>(a, cols, whole);
+  else
+    grouped_thin_kernel<T, RF, 4><<<(uint32_t)blocks, 256, 0, st>>>(a, cols, whole);
+  return hipGetLastError();
+}
+
 template <typename T>
 hipError_t product_typed(const GroupedArgs& a, bool transpose, hipStream_t st) {
   constexpr int CH = Matrix<T>::kChunk;
@@ -596,8 +718,20 @@ hipError_t product_typed(const GroupedArgs& a, bool transpose, hipStream_t st) {
   const int64_t blocks = tile_bound(a.rows, a.groups, kTile, cols);
   if (blocks > 0x7fffffff) return hipErrorInvalidConfiguration;
   const bool wide = whole_chunks<T>(a.x, a.ldx) && whole_chunks<T>(a.w, a.ldw) && a.ldg % CH == 0 && a.K % CH == 0 && a.N % CH == 0;
+  const bool tiled = sizeof(T) == 2 && wide && whole_chunks<T>(a.y, a.ldy);
+  if (!transpose) {
+    // Up to 8 rows a group the matrices are what takes time, and the kernel for few rows reads them as fast as any (64 groups of
+    // 1024 x 2048 in 16 bits, 64 rows 53 us, tiles 57; 512 rows 73 and 72; in 32 bits 72, tiles of 64 x 64 91).  Beyond, tiles read
+    // them less often (1,024 rows 89 and 72), but where there are few of them a good part of the chip has nothing to do (256 rows,
+    // 4 groups of 2048 x 2048 32 us, tiles 49).
+    const int side = tiled ? 256 : kTile;
+    const int64_t row_tiles = a.rows / side + a.groups, tiles = (row_tiles < a.rows ? row_tiles : a.rows) * ((a.N + side - 1) / side);
+    if (a.rows <= (int64_t)8 * a.groups) return thin_typed<T, 1>(a, st);
+    if (tiles < (tiled ? 128 : 512) && a.rows <= (int64_t)64 * a.groups)
+      return a.rows <= (int64_t)24 * a.groups ? thin_typed<T, 2>(a, st) : thin_typed<T, 4>(a, st);
+  }
   if constexpr (sizeof(T) == 2) {
-    if (wide && whole_chunks<T>(a.y, a.ldy)) {
+    if (tiled) {
       constexpr int BM = 256, BN = 256;
       const int wcols = (outc + BN - 1) / BN;
       const int64_t n = tile_bound(a.rows, a.groups, BM, wcols);
