@@ -339,13 +339,13 @@ __global__ __launch_bounds__(256) void e4m3_wide_kernel(E4m3Args a, int cols) {
 
 // ---- product, few rows a group -----------------------------------------------------------------------------------------------
 // As in 16 bits: every matrix that is met goes once from memory into the registers of the wave that needs it.  A wave has 16
-// columns and RF * 16 rows; KS of a workgroup's four waves share the columns, each with every KS-th run of two blocks of the
+// columns and RF * 16 rows; KS of a workgroup's waves (four, or KS if that is more) share the columns, each with every KS-th run of two blocks of the
 // contraction, and their sums are added in order.  Results of 32 bits take the numbers as bf16 (see above).
 constexpr int kThinRun = 2;
 
 template <typename T, int RF, int KS>
-__global__ __launch_bounds__(256) void e4m3_thin_kernel(E4m3Args a, int col_tiles, int whole_stores) {
-  constexpr int CT = 4 / KS;
+__global__ __launch_bounds__(KS > 4 ? KS * 64 : 256) void e4m3_thin_kernel(E4m3Args a, int col_tiles, int whole_stores) {
+  constexpr int CT = KS > 4 ? 1 : 4 / KS;
   constexpr bool WIDE = sizeof(T) == 4;
   __shared__ f32x4 part[KS > 1 ? (KS - 1) * CT * RF * 64 : 1];
   const RowTile t = find_tile<RF * 16>(a.offsets, a.groups, a.rows, col_tiles);
@@ -771,9 +771,12 @@ template <typename T, int RF>
 hipError_t thin_typed(const E4m3Args& a, hipStream_t st) {
   const int tiles = (a.N + 15) / 16;
   const int64_t met = a.rows < a.groups ? a.rows : a.groups;  // groups with rows, at most
-  // about 2,048 waves at work
-  const int ks = met * tiles >= 2048 ? 1 : met * tiles >= 1024 ? 2 : 4;
-  const int cols = (tiles + 4 / ks - 1) / (4 / ks);
+  // some 5,000 waves at work, few more than the chip holds at a time (64 rows, 64 groups of 1024 x 2048: one wave for its columns 27 us,
+  // two 24)
+  const int64_t waves = met * tiles;
+  const int ks = waves >= 5000 ? 1 : waves >= 2048 ? 2 : waves >= 1024 ? 4 : waves >= 512 || RF > 2 ? 8 : 16;
+  const int per_group = ks > 4 ? 1 : 4 / ks;
+  const int cols = (tiles + per_group - 1) / per_group;
   const int64_t blocks = tile_bound(a.rows, a.groups, RF * 16, cols);
   if (blocks > 0x7fffffff) return hipErrorInvalidConfiguration;
   const int whole = a.N % 4 == 0 && a.ldy % 4 == 0 && reinterpret_cast<uintptr_t>(a.y) % (4 * sizeof(T)) == 0;
@@ -781,8 +784,12 @@ hipError_t thin_typed(const E4m3Args& a, hipStream_t st) {
     e4m3_thin_kernel<T, RF, 1><<<(uint32_t)blocks, 256, 0, st>>>(a, cols, whole);
   else if (ks == 2)
     e4m3_thin_kernel<T, RF, 2><<<(uint32_t)blocks, 256, 0, st>>>(a, cols, whole);
-  else
+  else if (ks == 4)
     e4m3_thin_kernel<T, RF, 4><<<(uint32_t)blocks, 256, 0, st>>>(a, cols, whole);
+  else if (ks == 8)
+    e4m3_thin_kernel<T, RF, 8><<<(uint32_t)blocks, 512, 0, st>>>(a, cols, whole);
+  else if constexpr (RF <= 2)  // registers of 16 waves
+    e4m3_thin_kernel<T, RF, 16><<<(uint32_t)blocks, 1024, 0, st>>>(a, cols, whole);
   return hipGetLastError();
 }
 

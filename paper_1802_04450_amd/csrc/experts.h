@@ -57,7 +57,9 @@ struct GradientArgs {
   int groups, slots;
   int N, K;
   int dtype;
+  void* work;            // of grouped_gradient_workspace bytes, or null: then a group's rows are not cut
 };
+size_t grouped_gradient_workspace(int64_t rows, int groups, int N, int K, int dtype);
 hipError_t launch_grouped_gradient(const GradientArgs& a, hipStream_t st);
 
 // ---- e4m3.hip -------------------------------------------------------------------------------------------------------

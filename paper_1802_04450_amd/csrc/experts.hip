@@ -75,20 +75,22 @@ int sc_grouped_product(const void* x, int64_t ldx, int64_t n_x, const void* w, i
 int sc_grouped_gradient_workspace_bytes(int64_t rows, int32_t groups, int32_t N, int32_t K, int32_t dtype, size_t* bytes_out) {
   if (!bytes_out || rows < 0) return SC_EINVAL;
   if (!known_type(dtype) || !group_sizes(rows, rows, nullptr, 1, groups, N, K)) return SC_EDOMAIN;
-  *bytes_out = 0;
+  *bytes_out = grouped_gradient_workspace(rows, groups, N, K, dtype);
   return SC_OK;
 }
 
 int sc_grouped_gradient(const void* dy, int64_t lddy, const void* x, int64_t ldx, int64_t n_x, int32_t dtype,
                         const int32_t* offsets, const int32_t* order, int32_t slots, int64_t rows, int32_t groups, int32_t N,
                         int32_t K, void* dw_out, int64_t ldw, int64_t ldg, void* work, size_t work_bytes, void* stream) {
-  (void)work;
-  (void)work_bytes;
   if (rows < 0 || n_x < 0 || !offsets || !dw_out || (rows > 0 && (!dy || !x))) return SC_EINVAL;
   if (!known_type(dtype) || !group_sizes(rows, n_x, order, slots, groups, N, K) || lddy < N || ldx < K || ldw < K ||
       ldg < (int64_t)(N - 1) * ldw + K)
     return SC_EDOMAIN;
-  const GradientArgs a{dy, x, dw_out, offsets, order, lddy, ldx, ldw, ldg, rows, n_x, groups, order ? slots : 1, N, K, dtype};
+  const size_t need = grouped_gradient_workspace(rows, groups, N, K, dtype);
+  if (need > 0 && !work) return SC_EINVAL;
+  if (work_bytes < need || reinterpret_cast<uintptr_t>(work) % 16 != 0) return SC_EDOMAIN;
+  const GradientArgs a{dy, x, dw_out, offsets, order, lddy, ldx, ldw, ldg, rows, n_x, groups, order ? slots : 1, N, K, dtype,
+                       need > 0 ? work : nullptr};
   return status(launch_grouped_gradient(a, as_stream(stream)));
 }
 

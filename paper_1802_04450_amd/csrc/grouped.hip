@@ -39,156 +39,7 @@ struct Matrix<float> {
   }
 };
 
-// ---- any strides, any alignment ------------------------------------------------------------------------------------------
-// out(r, c) = sum over e of R(r, e) C(c, e), a 64 x 64 tile of out by four waves, 32 x 32 each.  The contraction goes through
-// LDS in steps of four chunks; the next step's chunks are loaded while this one's products run.
-constexpr int kTile = 64;
-
-enum { kProduct = 0, kTransposed = 1, kGradient = 2 };
-
-// Eight (four) consecutive values from p on, of which `left` exist.
-template <typename T, bool WIDE>
-__device__ __forceinline__ typename Matrix<T>::Chunk load_chunk(const T* p, int left) {
-  typedef typename Matrix<T>::Chunk Chunk;
-  constexpr int CH = Matrix<T>::kChunk;
-  Chunk v;
-#pragma unroll
-  for (int u = 0; u < CH; ++u) v[u] = static_cast<T>(0.0f);
-  if (left <= 0) return v;
-  if constexpr (WIDE) return *reinterpret_cast<const Chunk*>(p);  // lengths are whole chunks there
-#pragma unroll
-  for (int u = 0; u < CH; ++u)
-    if (u < left) v[u] = p[u];
-  return v;
-}
-
-template <typename T, int FORM, bool WIDE>
-__global__ __launch_bounds__(256) void grouped_any_kernel(const T* __restrict__ rmat, const T* __restrict__ cmat, T* __restrict__ out,
-                                                          const int32_t* __restrict__ offsets, const int32_t* __restrict__ order,
-                                                          int64_t ldr, int64_t ldc, int64_t ldg, int64_t ldo, int64_t ldog,
-                                                          int64_t rows, int64_t xrows, int groups, int slots, int outr, int outc,
-                                                          int depth, int row_tiles, int col_tiles) {
-  typedef typename Matrix<T>::Chunk Chunk;
-  constexpr int CH = Matrix<T>::kChunk;
-  constexpr int BK = 4 * CH;
-  constexpr int LD = BK + CH;  // a row of a tile in LDS: one chunk more, so that the rows do not all begin in one bank
-  __shared__ T rs[kTile * LD], cs[kTile * LD];
-  int group, r0, rn, c0;
-  int64_t pbegin = 0, pcount = 0;
-  if (FORM == kGradient) {
-    group = blockIdx.x / (row_tiles * col_tiles);
-    const int at = blockIdx.x - group * (row_tiles * col_tiles);
-    r0 = at / col_tiles * kTile;
-    c0 = at % col_tiles * kTile;
-    rn = min(kTile, outr - r0);
-    const GroupRange g = group_range(offsets, groups, rows, group);
-    pbegin = g.begin;
-    pcount = g.end - g.begin;
-  } else {
-    const RowTile t = find_tile<kTile>(offsets, groups, rows, col_tiles);
-    if (t.group < 0) return;
-    group = t.group;
-    r0 = 0;
-    pbegin = t.begin;
-    rn = t.count;
-    c0 = t.col * kTile;
-  }
-  const int cn = min(kTile, outc - c0);
-  const bool empty = FORM != kGradient && group == groups;
-  const int64_t length = empty ? 0 : (FORM == kGradient ? pcount : depth);
-  const T* cbase = FORM == kGradient || empty ? cmat : cmat + (int64_t)group * ldg;
-
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-  const int wr = (wave >> 1) * 32, wc = (wave & 1) * 32;
-  f32x4 acc[2][2];
-#pragma unroll
-  for (int a = 0; a < 2; ++a)
-#pragma unroll
-    for (int b = 0; b < 2; ++b) acc[a][b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-
-  // A thread's chunk: of row `tid / 4` where rows run along the contraction, else of step tid / (64 / CH) of the contraction.
-  constexpr int PER = kTile / CH;
-  const int along_row = tid >> 2, along_e = (tid & 3) * CH;
-  const int across_e = tid / PER, across_col = tid % PER * CH;
-  int64_t rrow = -1;
-  if (FORM != kGradient && along_row < rn) rrow = source_row(order, pbegin + along_row, slots, xrows);
-
-  auto load = [&](int64_t e0, Chunk& r, Chunk& c) {
-    if (FORM != kGradient) {
-      const int64_t e = e0 + along_e;
-      r = load_chunk<T, WIDE>(rmat + (rrow < 0 ? 0 : rrow * ldr + e), rrow < 0 ? 0 : (int)min((int64_t)CH, length - e));
-    } else {
-      const int64_t e = e0 + across_e;
-      const int left = e < length ? min(CH, outr - (r0 + across_col)) : 0;
-      r = load_chunk<T, WIDE>(rmat + (left > 0 ? (pbegin + e) * ldr + r0 + across_col : 0), left);
-    }
-    if (FORM == kProduct) {
-      const int64_t e = e0 + along_e;
-      const int left = along_row < cn ? (int)min((int64_t)CH, length - e) : 0;
-      c = load_chunk<T, WIDE>(cbase + (left > 0 ? (int64_t)(c0 + along_row) * ldc + e : 0), left);
-    } else {
-      const int64_t e = e0 + across_e;
-      int left = e < length ? min(CH, outc - (c0 + across_col)) : 0;
-      int64_t at = 0;
-      if (left > 0) {
-        at = FORM == kGradient ? source_row(order, pbegin + e, slots, xrows) : e;
-        if (at < 0) left = 0;
-      }
-      c = load_chunk<T, WIDE>(cbase + (left > 0 ? at * ldc + c0 + across_col : 0), left);
-    }
-  };
-  auto store = [&](T* tile, const Chunk& v, bool along) {
-    if (along) {
-      *reinterpret_cast<Chunk*>(tile + along_row * LD + along_e) = v;
-    } else {
-#pragma unroll
-      for (int u = 0; u < CH; ++u) tile[(across_col + u) * LD + across_e] = v[u];
-    }
-  };
-
-  Chunk r, c;
-  if (length > 0) load(0, r, c);
-  for (int64_t e0 = 0; e0 < length; e0 += BK) {
-    store(rs, r, FORM != kGradient);
-    store(cs, c, FORM == kProduct);
-    __syncthreads();
-    if (e0 + BK < length) load(e0 + BK, r, c);
-    Chunk fr[2], fc[2];
-#pragma unroll
-    for (int a = 0; a < 2; ++a) {
-      fr[a] = *reinterpret_cast<const Chunk*>(rs + (wr + a * 16 + (lane & 15)) * LD + (lane >> 4) * CH);
-      fc[a] = *reinterpret_cast<const Chunk*>(cs + (wc + a * 16 + (lane & 15)) * LD + (lane >> 4) * CH);
-    }
-#pragma unroll
-    for (int a = 0; a < 2; ++a)
-#pragma unroll
-      for (int b = 0; b < 2; ++b) acc[a][b] = Matrix<T>::mma(fc[b], fr[a], acc[a][b]);  // a lane gets four neighbours of a row
-    __syncthreads();
-  }
-
-  T* obase = FORM == kGradient ? out + (int64_t)group * ldog : out;
-#pragma unroll
-  for (int a = 0; a < 2; ++a) {
-    const int row = wr + a * 16 + (lane & 15);
-    if (row >= rn) continue;
-    T* orow = obase + ((FORM == kGradient ? (int64_t)r0 : pbegin) + row) * ldo + c0;
-#pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      const int col = wc + b * 16 + (lane >> 4) * 4;
-#pragma unroll
-      for (int u = 0; u < 4; ++u)
-        if (col + u < cn) orow[col + u] = static_cast<T>(acc[a][b][u]);
-    }
-  }
-}
-
-// ---- few rows a group ----------------------------------------------------------------------------------------------------------
-// Every matrix that is met is read once, from memory straight into the registers of the wave that needs it, and that is what
-// bounds it.  A wave has 16 columns and RF * 16 rows; KS of a workgroup's four waves share the columns, each with every KS-th
-// run of RUN chunks of the contraction, and their sums are added in order at the end: as few columns as there are, enough
-// waves are at work.  A run of the matrix is on its way while one is used.  Rows of any alignment: a lane's 16 bytes may begin anywhere.
-constexpr int kThinRun = 4;
-
+// A lane's 16 bytes of a row, which may begin anywhere, and of which `left` values exist.
 template <typename T>
 __device__ __forceinline__ typename Matrix<T>::Chunk load_any(const T* p, int64_t left) {
   typedef typename Matrix<T>::Chunk Chunk;
@@ -203,10 +54,246 @@ __device__ __forceinline__ typename Matrix<T>::Chunk load_any(const T* p, int64_
   return v;
 }
 
-template <typename T, int RF, int KS>
-__global__ __launch_bounds__(256) void grouped_thin_kernel(GroupedArgs a, int col_tiles, int whole_stores) {
+// ---- any strides, any alignment ------------------------------------------------------------------------------------------
+// out(r, c) = sum over e of R(r, e) C(c, e), a TILE x TILE tile of out by four waves, a quarter each.  The contraction goes through
+// two buffers of LDS in steps of 4 U chunks: the next step's chunks are loaded into registers while this one's products run.
+// An operand whose rows run along the contraction lies in LDS row by row; one whose rows run across it step by step, and the
+// values of a fragment are put together when they are read (16 bits: by the transposing read).
+enum { kProduct = 0, kTransposed = 1, kGradient = 2 };
+
+typedef short short4v __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) short4v LdsShort4;
+
+// Where a part of a gradient's contraction goes: the rows of a group are cut into parts of `part` (0: not at all), whose sums in
+// fp32 lie one after the other in `sums`, groups x their parts x N x K.
+struct Parts {
+  int part;
+  float* sums;
+};
+
+template <typename T, int FORM, int TILE, int U>
+__global__ __launch_bounds__(256) void grouped_any_kernel(const T* __restrict__ rmat, const T* __restrict__ cmat, T* __restrict__ out,
+                                                          const int32_t* __restrict__ offsets, const int32_t* __restrict__ order,
+                                                          int64_t ldr, int64_t ldc, int64_t ldg, int64_t ldo, int64_t ldog,
+                                                          int64_t rows, int64_t xrows, int groups, int slots, int outr, int outc,
+                                                          int depth, int row_tiles, int col_tiles, Parts parts, int whole_stores) {
   typedef typename Matrix<T>::Chunk Chunk;
-  constexpr int CH = Matrix<T>::kChunk, CT = 4 / KS, BK = 4 * CH;
+  constexpr int CH = Matrix<T>::kChunk;
+  constexpr int BK = 4 * CH * U;
+  constexpr bool R_ALONG = FORM != kGradient, C_ALONG = FORM == kProduct;
+  // rows of a tile in LDS, so that the rows read at one time do not all begin in one bank
+  constexpr int ALONG = BK + CH, ACROSS = TILE + 2 * CH;
+  constexpr int RSIZE = R_ALONG ? TILE * ALONG : BK * ACROSS, CSIZE = C_ALONG ? TILE * ALONG : BK * ACROSS;
+  constexpr int LOADS = TILE * BK / CH / 256, F = TILE / 32;
+  __shared__ __attribute__((aligned(16))) T lds[2][RSIZE + CSIZE];
+  int group, r0 = 0, rn, c0;
+  int64_t pbegin = 0, length;
+  float* sums = nullptr;
+  if (FORM == kGradient) {
+    const int per = row_tiles * col_tiles;
+    const int index = blockIdx.x / per, in = blockIdx.x - index * per;
+    r0 = in / col_tiles * TILE;
+    c0 = in % col_tiles * TILE;
+    rn = min(TILE, outr - r0);
+    if (parts.part) {
+      const RowTile t = part_at(offsets, groups, rows, parts.part, index);
+      if (t.group < 0) return;
+      group = t.group;
+      pbegin = t.begin;
+      length = t.count;
+      sums = parts.sums + ((int64_t)index * outr + r0) * outc + c0;
+    } else {
+      group = index;
+      const GroupRange g = group_range(offsets, groups, rows, group);
+      pbegin = g.begin;
+      length = g.end - g.begin;
+    }
+  } else {
+    const RowTile t = find_tile<TILE>(offsets, groups, rows, col_tiles);
+    if (t.group < 0) return;
+    group = t.group;
+    pbegin = t.begin;
+    rn = t.count;
+    c0 = t.col * TILE;
+    length = group == groups ? 0 : depth;
+  }
+  const int cn = min(TILE, outc - c0);
+  const T* cbase = FORM == kGradient || length == 0 ? cmat : cmat + (int64_t)group * ldg;
+
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+  const int sub = lane & 15, quad = lane >> 4;
+  const int wr = (wave >> 1) * (TILE / 2), wc = (wave & 1) * (TILE / 2);
+  f32x4 acc[F][F];
+#pragma unroll
+  for (int a = 0; a < F; ++a)
+#pragma unroll
+    for (int b = 0; b < F; ++b) acc[a][b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+
+  // A thread's chunks, LOADS of each operand: chunk i is piece i % (BK / CH) of row i / (BK / CH), or, across, piece i % (TILE / CH) of
+  // step i / (TILE / CH).
+  auto along_row = [&](int u) { return (tid + u * 256) / (BK / CH); };
+  auto along_e = [&](int u) { return (tid + u * 256) % (BK / CH) * CH; };
+  auto across_e = [&](int u) { return (tid + u * 256) / (TILE / CH); };
+  auto across_col = [&](int u) { return (tid + u * 256) % (TILE / CH) * CH; };
+  const T *rp[LOADS], *cp[LOADS];
+  int look[LOADS];
+#pragma unroll
+  for (int u = 0; u < LOADS; ++u) {
+    rp[u] = cp[u] = nullptr;  // nothing there
+    if (R_ALONG) {
+      const int64_t src = along_row(u) < rn && length > 0 ? source_row(order, pbegin + along_row(u), slots, xrows) : -1;
+      if (src >= 0) rp[u] = rmat + src * ldr + along_e(u);
+    } else if (across_col(u) < rn) {
+      rp[u] = rmat + (pbegin + across_e(u)) * ldr + r0 + across_col(u);
+    }
+    if (C_ALONG) {
+      if (along_row(u) < cn) cp[u] = cbase + (int64_t)(c0 + along_row(u)) * ldc + along_e(u);
+    } else if (across_col(u) < cn) {
+      cp[u] = cbase + (FORM == kGradient ? 0 : across_e(u) * ldc) + c0 + across_col(u);
+    }
+  }
+  auto look_up = [&](int64_t e0) {  // gradient: the rows of x that the next step takes
+    if (FORM == kGradient) {
+#pragma unroll
+      for (int u = 0; u < LOADS; ++u) {
+        const int64_t e = e0 + across_e(u);
+        look[u] = e < length ? (int)source_row(order, pbegin + e, slots, xrows) : -1;
+      }
+    }
+  };
+  auto load = [&](int64_t e0, Chunk (&r)[LOADS], Chunk (&c)[LOADS]) {
+#pragma unroll
+    for (int u = 0; u < LOADS; ++u) {
+      if (R_ALONG)
+        r[u] = load_any<T>(rp[u] + e0, rp[u] ? length - e0 - along_e(u) : 0);
+      else
+        r[u] = load_any<T>(rp[u] + e0 * ldr, rp[u] && e0 + across_e(u) < length ? rn - across_col(u) : 0);
+      if (C_ALONG)
+        c[u] = load_any<T>(cp[u] + e0, cp[u] ? length - e0 - along_e(u) : 0);
+      else if (FORM == kGradient)
+        c[u] = load_any<T>(cp[u] + (look[u] < 0 ? 0 : look[u]) * ldc, cp[u] && look[u] >= 0 ? cn - across_col(u) : 0);
+      else
+        c[u] = load_any<T>(cp[u] + e0 * ldc, cp[u] && e0 + across_e(u) < length ? cn - across_col(u) : 0);
+    }
+  };
+  auto put = [&](T* tile, bool along, const Chunk (&v)[LOADS]) {
+#pragma unroll
+    for (int u = 0; u < LOADS; ++u)
+      *reinterpret_cast<Chunk*>(along ? tile + along_row(u) * ALONG + along_e(u) : tile + across_e(u) * ACROSS + across_col(u)) = v[u];
+  };
+  // Rows (columns) first ... first + 15 of an operand, the kk-th 4 chunks of the step.
+  auto fragment = [&](const T* tile, bool along, int first, int kk) {
+    if (along) return *reinterpret_cast<const Chunk*>(tile + (first + sub) * ALONG + (kk * 4 + quad) * CH);
+    const int e = (kk * 4 + quad) * CH;
+    Chunk f;
+    if constexpr (sizeof(T) == 2) {
+      union {
+        short4v half[2];
+        Chunk whole;
+      } u;
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        u.half[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsShort4*)(tile + (e + h * 4 + (sub >> 2)) * ACROSS + first + (sub & 3) * 4));
+      f = u.whole;
+    } else {
+#pragma unroll
+      for (int j = 0; j < CH; ++j) f[j] = tile[(e + j) * ACROSS + first + sub];
+    }
+    return f;
+  };
+
+  Chunk r[LOADS], c[LOADS];
+  if (length > 0) {
+    look_up(0);
+    load(0, r, c);
+    look_up(BK);
+  }
+  int now = 0;
+  for (int64_t e0 = 0; e0 < length; e0 += BK) {
+    T* rt = lds[now];
+    T* ct = lds[now] + RSIZE;
+    put(rt, R_ALONG, r);
+    put(ct, C_ALONG, c);
+    __syncthreads();  // the other buffer has been read by all by then
+    if (e0 + BK < length) {
+      load(e0 + BK, r, c);
+      look_up(e0 + 2 * BK);
+    }
+#pragma unroll
+    for (int kk = 0; kk < U; ++kk) {
+      Chunk fr[F], fc[F];
+#pragma unroll
+      for (int a = 0; a < F; ++a) {
+        fr[a] = fragment(rt, R_ALONG, wr + a * 16, kk);
+        fc[a] = fragment(ct, C_ALONG, wc + a * 16, kk);
+      }
+#pragma unroll
+      for (int a = 0; a < F; ++a)
+#pragma unroll
+        for (int b = 0; b < F; ++b) acc[a][b] = Matrix<T>::mma(fc[b], fr[a], acc[a][b]);  // a lane gets four neighbours of a row
+    }
+    now ^= 1;
+  }
+
+  T* obase = FORM == kGradient ? out + (int64_t)group * ldog : out;
+#pragma unroll
+  for (int a = 0; a < F; ++a) {
+    const int row = wr + a * 16 + sub;
+    if (row >= rn) continue;
+    T* orow = obase + ((FORM == kGradient ? (int64_t)r0 : pbegin) + row) * ldo + c0;
+#pragma unroll
+    for (int b = 0; b < F; ++b) {
+      const int col = wc + b * 16 + quad * 4;
+      if (col >= cn) continue;
+      if (FORM == kGradient && sums) {
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+          if (col + u < cn) sums[(int64_t)row * outc + col + u] = acc[a][b][u];
+        continue;
+      }
+      typedef T Quad __attribute__((ext_vector_type(4)));
+      Quad q;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) q[u] = static_cast<T>(acc[a][b][u]);
+      if (whole_stores) {
+        *reinterpret_cast<Quad*>(orow + col) = q;
+      } else {
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+          if (col + u < cn) orow[col + u] = q[u];
+      }
+    }
+  }
+}
+
+// dw_g = the sums of group g's parts, in their order.
+template <typename T>
+__global__ __launch_bounds__(256) void gradient_sum_kernel(Parts parts, const int32_t* __restrict__ offsets, int groups, int64_t rows,
+                                                           int g0, int N, int K, T* __restrict__ dw, int64_t ldw,
+                                                           int64_t ldg) {
+  const int g = g0 + blockIdx.y;
+  const int64_t size = (int64_t)N * K;
+  int first, count;
+  parts_of(offsets, groups, rows, parts.part, g, first, count);
+  const float* sums = parts.sums + first * size;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < size; i += (int64_t)gridDim.x * 256) {
+    float sum = 0.0f;
+    for (int p = 0; p < count; ++p) sum += sums[p * size + i];
+    dw[(int64_t)g * ldg + i / K * ldw + i % K] = static_cast<T>(sum);
+  }
+}
+
+// ---- few rows a group ----------------------------------------------------------------------------------------------------------
+// Every matrix that is met is read once, from memory straight into the registers of the wave that needs it, and that is what
+// bounds it.  A wave has 16 columns and RF * 16 rows; KS of a workgroup's four waves share the columns, each with every KS-th
+// run of RUN chunks of the contraction, and their sums are added in order at the end: as few columns as there are, enough
+// waves are at work.  A run of the matrix is on its way while one is used.  Rows of any alignment: a lane's 16 bytes may begin anywhere.
+constexpr int kThinRun = 4;
+
+template <typename T, int RF, int KS>
+__global__ __launch_bounds__(KS > 4 ? KS * 64 : 256) void grouped_thin_kernel(GroupedArgs a, int col_tiles, int whole_stores) {
+  typedef typename Matrix<T>::Chunk Chunk;
+  constexpr int CH = Matrix<T>::kChunk, CT = KS > 4 ? 1 : 4 / KS, BK = 4 * CH;
   __shared__ f32x4 part[KS > 1 ? (KS - 1) * CT * RF * 64 : 1];
   const RowTile t = find_tile<RF * 16>(a.offsets, a.groups, a.rows, col_tiles);
   if (t.group < 0) return;
@@ -295,8 +382,6 @@ __global__ __launch_bounds__(256) void grouped_thin_kernel(GroupedArgs a, int co
 // permuted.
 __device__ uint4 zero_piece[1];
 
-typedef short short4v __attribute__((ext_vector_type(4)));
-typedef __attribute__((address_space(3))) short4v LdsShort4;
 
 // 16 bytes a lane from src to dst + 16 * lane, dst the same for the wave.  Written as an instruction of its own because the compiler
 // counts the builtin as an access that may return out of order and then waits for every LDS read at once; it returns nothing in a
@@ -343,7 +428,7 @@ template <typename T, int FORM, int BM, int BN, int WR, int WC>
 __global__ __launch_bounds__(WR * WC * 64) void grouped_tile_kernel(
     const T* __restrict__ rmat, const T* __restrict__ cmat, T* __restrict__ out, const int32_t* __restrict__ offsets,
     const int32_t* __restrict__ order, int64_t ldr, int64_t ldc, int64_t ldg, int64_t ldo, int64_t ldog, int64_t rows,
-    int64_t xrows, int groups, int slots, int outr, int outc, int depth, int row_tiles, int col_tiles) {
+    int64_t xrows, int groups, int slots, int outr, int outc, int depth, int row_tiles, int col_tiles, Parts parts) {
   typedef typename Matrix<T>::Chunk Chunk;
   typedef T Part __attribute__((ext_vector_type(8)));
   constexpr int NW = WR * WC;
@@ -365,24 +450,33 @@ __global__ __launch_bounds__(WR * WC * 64) void grouped_tile_kernel(
     int length;
   };
   const TileWalk<BM> walk(offsets, FORM == kGradient ? 0 : groups, rows, FORM == kGradient ? 1 : col_tiles);
-  const GroupOrder by_length(offsets, FORM == kGradient ? groups : 0, rows);
+  const GroupOrder by_length(offsets, FORM == kGradient && !parts.part ? groups : 0, rows);
+  const PartList part_list(offsets, FORM == kGradient && parts.part ? groups : 0, rows, parts.part);
+  const int64_t group_parts = FORM != kGradient ? 0 : parts.part ? part_list.total : groups;
   const int per_group = row_tiles * col_tiles;  // gradient
   // A gradient's tiles take as long as their groups are.  From the longest group to the shortest they are dealt out to all
   // workgroups, to and fro.
   const int64_t count =
-      FORM == kGradient ? ((int64_t)groups * per_group + gridDim.x - 1) / gridDim.x : walk.count;
+      FORM == kGradient ? (group_parts * per_group + gridDim.x - 1) / gridDim.x : walk.count;
   auto tile_at = [&](int64_t i, Tile& t) {  // false: there is none (only the last one of a gradient)
     if (FORM == kGradient) {
       const int64_t at = i * gridDim.x + (i & 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
-      if (at >= (int64_t)groups * per_group) return false;
+      if (at >= group_parts * per_group) return false;
       const int g = (int)(at / per_group), in = (int)(at - (int64_t)g * per_group);
-      t.group = by_length.at(g);
       t.r0 = in / col_tiles * BM;
       t.c0 = in % col_tiles * BN;
       t.rn = min(BM, outr - t.r0);
-      const GroupRange r = group_range(offsets, groups, rows, t.group);
-      t.pbegin = r.begin;
-      t.length = (int)(r.end - r.begin);
+      if (parts.part) {
+        const RowTile r = part_list.at(g);
+        t.group = g;  // the part's number: where its sums go
+        t.pbegin = r.begin;
+        t.length = r.count;
+      } else {
+        t.group = by_length.at(g);
+        const GroupRange r = group_range(offsets, groups, rows, t.group);
+        t.pbegin = r.begin;
+        t.length = (int)(r.end - r.begin);
+      }
     } else {
       const RowTile r = walk.at(i);
       t.group = r.group;
@@ -508,6 +602,15 @@ __global__ __launch_bounds__(WR * WC * 64) void grouped_tile_kernel(
       const int row = wr + a * 16 + sub;
       if (row >= t.rn) continue;
       T* orow = base + row * ldo + t.c0;
+      if (FORM == kGradient && parts.part) {
+        float* sums = parts.sums + ((int64_t)t.group * outr + t.r0 + row) * outc + t.c0;
+#pragma unroll
+        for (int b = 0; b < FC; ++b) {
+          const int col = wc + fragment_col(b, quad * 4);
+          if (col < t.cn) *reinterpret_cast<f32x4*>(sums + col) = acc[a][b];
+        }
+        continue;
+      }
       const bool none = FORM != kGradient && order && (uint32_t)order[t.pbegin + row] >= known;  // a row of zeros
 #pragma unroll
       for (int b = 0; b < FC; b += 2) {
@@ -693,9 +796,12 @@ template <typename T, int RF>
 hipError_t thin_typed(const GroupedArgs& a, hipStream_t st) {
   const int tiles = (a.N + 15) / 16;
   const int64_t met = a.rows < a.groups ? a.rows : a.groups;  // groups with rows, at most
-  // about 2,048 waves at work
-  const int ks = met * tiles >= 2048 ? 1 : met * tiles >= 1024 ? 2 : 4;
-  const int cols = (tiles + 4 / ks - 1) / (4 / ks);
+  // some 5,000 waves at work, few more than the chip holds at a time (64 rows, 64 groups of 1024 x 2048: one wave for its columns 59 us,
+  // two 46, four 48; 1 row of 2048 x 2048: four 10.8, sixteen ...)
+  const int64_t waves = met * tiles;
+  const int ks = waves >= 5000 ? 1 : waves >= 2048 ? 2 : waves >= 1024 ? 4 : waves >= 512 || RF > 2 ? 8 : 16;
+  const int per_group = ks > 4 ? 1 : 4 / ks;
+  const int cols = (tiles + per_group - 1) / per_group;
   const int64_t blocks = tile_bound(a.rows, a.groups, RF * 16, cols);
   if (blocks > 0x7fffffff) return hipErrorInvalidConfiguration;
   const int whole = a.N % 4 == 0 && a.ldy % 4 == 0 && reinterpret_cast<uintptr_t>(a.y) % (4 * sizeof(T)) == 0;
@@ -703,8 +809,27 @@ hipError_t thin_typed(const GroupedArgs& a, hipStream_t st) {
     grouped_thin_kernel<T, RF, 1><<<(uint32_t)blocks, 256, 0, st>>>(a, cols, whole);
   else if (ks == 2)
     grouped_thin_kernel<T, RF, 2><<<(uint32_t)blocks, 256, 0, st>>>(a, cols, whole);
-  else
+  else if (ks == 4)
     grouped_thin_kernel<T, RF, 4><<<(uint32_t)blocks, 256, 0, st>>>(a, cols, whole);
+  else if (ks == 8)
+    grouped_thin_kernel<T, RF, 8><<<(uint32_t)blocks, 512, 0, st>>>(a, cols, whole);
+  else if constexpr (RF <= 2)  // registers of 16 waves
+    grouped_thin_kernel<T, RF, 16><<<(uint32_t)blocks, 1024, 0, st>>>(a, cols, whole);
+  return hipGetLastError();
+}
+
+// Tiles of a general kernel: 128 x 128 where there are enough of them, else 64 x 64.
+bool large_tiles(int64_t row_tiles_128, int64_t cols, int row_parts = 1) { return row_tiles_128 * ((cols + 127) / 128) * row_parts >= 512; }
+
+template <typename T, int FORM, int TILE>
+hipError_t any_typed(const GroupedArgs& a, int outc, int depth, hipStream_t st) {
+  const int cols = (outc + TILE - 1) / TILE;
+  const int64_t blocks = tile_bound(a.rows, a.groups, TILE, cols);
+  if (blocks > 0x7fffffff) return hipErrorInvalidConfiguration;
+  const int whole = outc % 4 == 0 && a.ldy % 4 == 0 && reinterpret_cast<uintptr_t>(a.y) % (4 * sizeof(T)) == 0;
+  grouped_any_kernel<T, FORM, TILE, TILE == 64 ? 2 : 1><<<(uint32_t)blocks, 256, 0, st>>>(
+      static_cast<const T*>(a.x), static_cast<const T*>(a.w), static_cast<T*>(a.y), a.offsets, a.order, a.ldx, a.ldw, a.ldg, a.ldy, 0,
+      a.rows, a.xrows, a.groups, a.slots, 0, outc, depth, 0, cols, Parts{0, nullptr}, whole);
   return hipGetLastError();
 }
 
@@ -712,19 +837,14 @@ template <typename T>
 hipError_t product_typed(const GroupedArgs& a, bool transpose, hipStream_t st) {
   constexpr int CH = Matrix<T>::kChunk;
   const int outc = transpose ? a.K : a.N, depth = transpose ? a.N : a.K;
-  const T *x = static_cast<const T*>(a.x), *w = static_cast<const T*>(a.w);
-  T* y = static_cast<T*>(a.y);
-  const int cols = (outc + kTile - 1) / kTile;
-  const int64_t blocks = tile_bound(a.rows, a.groups, kTile, cols);
-  if (blocks > 0x7fffffff) return hipErrorInvalidConfiguration;
-  const bool wide = whole_chunks<T>(a.x, a.ldx) && whole_chunks<T>(a.w, a.ldw) && a.ldg % CH == 0 && a.K % CH == 0 && a.N % CH == 0;
-  const bool tiled = sizeof(T) == 2 && wide && whole_chunks<T>(a.y, a.ldy);
+  const bool tiled = sizeof(T) == 2 && whole_chunks<T>(a.x, a.ldx) && whole_chunks<T>(a.w, a.ldw) && a.ldg % CH == 0 &&
+                     a.K % CH == 0 && a.N % CH == 0 && whole_chunks<T>(a.y, a.ldy);
   if (!transpose) {
     // Up to 8 rows a group the matrices are what takes time, and the kernel for few rows reads them as fast as any (64 groups of
     // 1024 x 2048 in 16 bits, 64 rows 53 us, tiles 57; 512 rows 73 and 72; in 32 bits 72, tiles of 64 x 64 91).  Beyond, tiles read
     // them less often (1,024 rows 89 and 72), but where there are few of them a good part of the chip has nothing to do (256 rows,
     // 4 groups of 2048 x 2048 32 us, tiles 49).
-    const int side = tiled ? 256 : kTile;
+    const int side = tiled ? 256 : 64;
     const int64_t row_tiles = a.rows / side + a.groups, tiles = (row_tiles < a.rows ? row_tiles : a.rows) * ((a.N + side - 1) / side);
     if (a.rows <= (int64_t)8 * a.groups) return thin_typed<T, 1>(a, st);
     if (tiles < (tiled ? 128 : 512) && a.rows <= (int64_t)64 * a.groups)
@@ -733,56 +853,106 @@ hipError_t product_typed(const GroupedArgs& a, bool transpose, hipStream_t st) {
   if constexpr (sizeof(T) == 2) {
     if (tiled) {
       constexpr int BM = 256, BN = 256;
+      const T *x = static_cast<const T*>(a.x), *w = static_cast<const T*>(a.w);
+      T* y = static_cast<T*>(a.y);
       const int wcols = (outc + BN - 1) / BN;
       const int64_t n = tile_bound(a.rows, a.groups, BM, wcols);
       const uint32_t grid = (uint32_t)(n < 256 ? n : 256);
       if (transpose)
         grouped_tile_kernel<T, kTransposed, BM, BN, 2, 4><<<grid, 512, 0, st>>>(
-            x, w, y, a.offsets, a.order, a.ldx, a.ldw, a.ldg, a.ldy, 0, a.rows, a.xrows, a.groups, a.slots, 0, outc, depth, 0, wcols);
+            x, w, y, a.offsets, a.order, a.ldx, a.ldw, a.ldg, a.ldy, 0, a.rows, a.xrows, a.groups, a.slots, 0, outc, depth, 0, wcols,
+            Parts{0, nullptr});
       else
         grouped_tile_kernel<T, kProduct, BM, BN, 2, 4><<<grid, 512, 0, st>>>(
-            x, w, y, a.offsets, a.order, a.ldx, a.ldw, a.ldg, a.ldy, 0, a.rows, a.xrows, a.groups, a.slots, 0, outc, depth, 0, wcols);
+            x, w, y, a.offsets, a.order, a.ldx, a.ldw, a.ldg, a.ldy, 0, a.rows, a.xrows, a.groups, a.slots, 0, outc, depth, 0, wcols,
+            Parts{0, nullptr});
       return hipGetLastError();
     }
   }
-#define SC_LAUNCH(FORM, WIDE)                                                                                                   \
-  grouped_any_kernel<T, FORM, WIDE><<<(uint32_t)blocks, 256, 0, st>>>(x, w, y, a.offsets, a.order, a.ldx, a.ldw, a.ldg, a.ldy, 0, \
-                                                                      a.rows, a.xrows, a.groups, a.slots, 0, outc, depth, 0, cols)
-  if (transpose && wide) SC_LAUNCH(kTransposed, true);
-  else if (transpose) SC_LAUNCH(kTransposed, false);
-  else if (wide) SC_LAUNCH(kProduct, true);
-  else SC_LAUNCH(kProduct, false);
-#undef SC_LAUNCH
+  const bool large = large_tiles(a.rows / 128, outc);
+  if (transpose) return large ? any_typed<T, kTransposed, 128>(a, outc, depth, st) : any_typed<T, kTransposed, 64>(a, outc, depth, st);
+  return large ? any_typed<T, kProduct, 128>(a, outc, depth, st) : any_typed<T, kProduct, 64>(a, outc, depth, st);
+}
+
+// How a gradient's rows are cut: rows a part (0: not), parts at most.  Where the tiles of all groups are fewer than the chip takes, a
+// group's rows go in parts, so many that the workgroups there are have something to do and not more: their sums are written
+// and read once more.
+struct GradientCut {
+  int side;  // tiles
+  int64_t tiles;  // of one group
+  int part;
+  int64_t parts;
+};
+GradientCut gradient_cut(int64_t rows, int groups, int N, int K, int dtype) {
+  GradientCut c;
+  const bool tiled = dtype != kF32 && N % 8 == 0 && K % 8 == 0;
+  const int64_t small = (int64_t)((N + 63) / 64) * ((K + 63) / 64), large = (int64_t)((N + 127) / 128) * ((K + 127) / 128),
+                huge = (int64_t)((N + 255) / 256) * ((K + 255) / 256);
+  // 256 x 256 tiles want rows enough for all workgroups to have some steps; else the smaller the more workgroups
+  if (tiled && huge * (rows / 512 + groups) >= 128)
+    c.side = 256, c.tiles = huge;
+  else if (large * (rows / 512 + groups) >= 512)
+    c.side = 128, c.tiles = large;
+  else
+    c.side = 64, c.tiles = small;
+  const int64_t want = c.side == 256 ? 256 : c.side == 128 ? 1024 : 2048;  // workgroups
+  c.part = 0;
+  c.parts = 0;
+  if (groups * c.tiles < want && rows > 256) {
+    int64_t part = rows * c.tiles / want;
+    part = part < 128 ? 128 : (part + 63) / 64 * 64;
+    if (part < rows) {
+      c.part = (int)part;
+      c.parts = rows / part + groups;
+    }
+  }
+  return c;
+}
+
+template <typename T, int TILE>
+hipError_t any_gradient(const GradientArgs& a, const GradientCut& c, const Parts& parts, hipStream_t st) {
+  const int rt = (a.N + TILE - 1) / TILE, ct = (a.K + TILE - 1) / TILE;
+  const int64_t blocks = (c.part ? c.parts : a.groups) * rt * ct;
+  if (blocks > 0x7fffffff) return hipErrorInvalidConfiguration;
+  const int whole = a.K % 4 == 0 && a.ldw % 4 == 0 && a.ldg % 4 == 0 && reinterpret_cast<uintptr_t>(a.dw) % (4 * sizeof(T)) == 0;
+  grouped_any_kernel<T, kGradient, TILE, TILE == 64 ? 2 : 1><<<(uint32_t)blocks, 256, 0, st>>>(
+      static_cast<const T*>(a.dy), static_cast<const T*>(a.x), static_cast<T*>(a.dw), a.offsets, a.order, a.lddy, a.ldx, 0, a.ldw,
+      a.ldg, a.rows, a.xrows, a.groups, a.slots, a.N, a.K, 0, rt, ct, parts, whole);
   return hipGetLastError();
 }
 
 template <typename T>
 hipError_t gradient_typed(const GradientArgs& a, hipStream_t st) {
   constexpr int CH = Matrix<T>::kChunk;
-  const T *dy = static_cast<const T*>(a.dy), *x = static_cast<const T*>(a.x);
-  T* dw = static_cast<T*>(a.dw);
-  const int rt = (a.N + kTile - 1) / kTile, ct = (a.K + kTile - 1) / kTile;
-  const int64_t blocks = (int64_t)a.groups * rt * ct;
-  if (blocks > 0x7fffffff) return hipErrorInvalidConfiguration;
-  const bool wide = whole_chunks<T>(a.x, a.ldx) && whole_chunks<T>(a.dy, a.lddy) && a.K % CH == 0 && a.N % CH == 0;
+  GradientCut c = gradient_cut(a.rows, a.groups, a.N, a.K, a.dtype);
+  if (c.part && !a.work) c.part = 0;
+  const Parts parts{c.part, c.part ? static_cast<float*>(a.work) : nullptr};
+  const bool tiled = sizeof(T) == 2 && whole_chunks<T>(a.x, a.ldx) && whole_chunks<T>(a.dy, a.lddy) && a.K % CH == 0 &&
+                     a.N % CH == 0 && whole_chunks<T>(a.dw, a.ldw) && a.ldg % CH == 0;
+  hipError_t e = hipSuccess;
+  bool done = false;
   if constexpr (sizeof(T) == 2) {
-    if (wide && whole_chunks<T>(a.dw, a.ldw) && a.ldg % CH == 0) {
-      constexpr int BM = 256, BN = 256;
-      const int wr = (a.N + BM - 1) / BM, wc = (a.K + BN - 1) / BN;
-      const int64_t n = (int64_t)a.groups * wr * wc;
-      grouped_tile_kernel<T, kGradient, BM, BN, 2, 4><<<(uint32_t)(n < 256 ? n : 256), 512, 0, st>>>(
-          dy, x, dw, a.offsets, a.order, a.lddy, a.ldx, 0, a.ldw, a.ldg, a.rows, a.xrows, a.groups, a.slots, a.N, a.K, 0, wr, wc);
-      return hipGetLastError();
+    if (tiled && c.side == 256) {
+      const int wr = (a.N + 255) / 256, wc = (a.K + 255) / 256;
+      const int64_t n = (c.part ? c.parts : a.groups) * wr * wc;
+      grouped_tile_kernel<T, kGradient, 256, 256, 2, 4><<<(uint32_t)(n < 256 ? n : 256), 512, 0, st>>>(
+          static_cast<const T*>(a.dy), static_cast<const T*>(a.x), static_cast<T*>(a.dw), a.offsets, a.order, a.lddy, a.ldx, 0, a.ldw,
+          a.ldg, a.rows, a.xrows, a.groups, a.slots, a.N, a.K, 0, wr, wc, parts);
+      e = hipGetLastError();
+      done = true;
     }
   }
-#define SC_LAUNCH(WIDE)                                                                                                        \
-  grouped_any_kernel<T, kGradient, WIDE><<<(uint32_t)blocks, 256, 0, st>>>(dy, x, dw, a.offsets, a.order, a.lddy, a.ldx, 0, a.ldw, \
-                                                                           a.ldg, a.rows, a.xrows, a.groups, a.slots, a.N, a.K, 0, \
-                                                                           rt, ct)
-  if (wide) SC_LAUNCH(true);
-  else SC_LAUNCH(false);
-#undef SC_LAUNCH
-  return hipGetLastError();
+  if (!done) e = c.side >= 128 ? any_gradient<T, 128>(a, c, parts, st) : any_gradient<T, 64>(a, c, parts, st);
+  if (e != hipSuccess || !c.part) return e;
+  const int64_t size = (int64_t)a.N * a.K, blocks = (size + 255) / 256;
+  for (int g0 = 0; g0 < a.groups; g0 += 65535) {
+    const int n = a.groups - g0 < 65535 ? a.groups - g0 : 65535;
+    gradient_sum_kernel<T><<<dim3((uint32_t)(blocks < 4096 ? blocks : 4096), n), 256, 0, st>>>(
+        parts, a.offsets, a.groups, a.rows, g0, a.N, a.K, static_cast<T*>(a.dw), a.ldw, a.ldg);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 }  // namespace
@@ -792,6 +962,10 @@ hipError_t launch_grouped_product(const GroupedArgs& a, bool transpose, hipStrea
   if (a.dtype == kF32) return product_typed<float>(a, transpose, st);
   if (a.dtype == kBF16) return product_typed<__bf16>(a, transpose, st);
   return product_typed<_Float16>(a, transpose, st);
+}
+
+size_t grouped_gradient_workspace(int64_t rows, int groups, int N, int K, int dtype) {
+  return sizeof(float) * (size_t)gradient_cut(rows, groups, N, K, dtype).parts * N * K;
 }
 
 hipError_t launch_grouped_gradient(const GradientArgs& a, hipStream_t st) {

@@ -140,6 +140,65 @@ struct TileWalk {
   }
 };
 
+// The rows of all groups in parts of `part`, numbered in order.
+struct PartList {
+  const int32_t* offsets;
+  int64_t rows;
+  int groups, per, part;
+  int mine, sum;  // parts of this lane's groups; of those of the lanes up to it
+  int total;
+
+  __device__ __forceinline__ PartList(const int32_t* o, int g, int64_t r, int p) : offsets(o), rows(r), groups(g), part(p) {
+    const int lane = threadIdx.x & 63;
+    per = (groups + 63) / 64;
+    mine = 0;
+    for (int u = 0; u < per; ++u) {
+      if (lane * per + u >= groups) break;
+      const GroupRange range = group_range(offsets, groups, rows, lane * per + u);
+      mine += (int)((range.end - range.begin + part - 1) / part);
+    }
+    sum = mine;
+#pragma unroll
+    for (int s = 1; s < 64; s <<= 1) {
+      const int v = __shfl_up(sum, s);
+      if (lane >= s) sum += v;
+    }
+    total = __builtin_amdgcn_readlane(sum, 63);
+  }
+  __device__ __forceinline__ RowTile at(int i) const {  // group -1 from the total on
+    RowTile t;
+    t.group = -1;
+    t.begin = 0;
+    t.count = 0;
+    t.col = 0;
+    if (i >= total) return t;
+    const int owner = __ffsll((unsigned long long)__ballot(i < sum)) - 1;
+    int left = i - __builtin_amdgcn_readlane(sum - mine, owner);
+    for (int g = owner * per; g < groups; ++g) {
+      const GroupRange r = group_range(offsets, groups, rows, g);
+      const int n = (int)((r.end - r.begin + part - 1) / part);
+      if (left < n) {
+        t.group = g;
+        t.begin = r.begin + (int64_t)left * part;
+        t.count = (int)min(r.end - t.begin, (int64_t)part);
+        break;
+      }
+      left -= n;
+    }
+    return t;
+  }
+};
+__device__ __forceinline__ RowTile part_at(const int32_t* offsets, int groups, int64_t rows, int part, int i) {
+  return PartList(offsets, groups, rows, part).at(i);
+}
+// The first part of group g and how many it has.
+__device__ __forceinline__ void parts_of(const int32_t* offsets, int groups, int64_t rows, int part, int g, int& first, int& count) {
+  const PartList list(offsets, g, rows, part);  // of the groups before
+  first = list.total;
+  const GroupRange r = group_range(offsets, groups, rows, g);
+  count = (int)((r.end - r.begin + part - 1) / part);
+}
+
 // The groups from the longest to the shortest, up to 64 of them; as they come if there are more.
 struct GroupOrder {
   int mine;  // of up to 64: the group whose place is the lane's number
