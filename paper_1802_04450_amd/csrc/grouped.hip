@@ -376,59 +376,56 @@ __global__ __launch_bounds__(KS > 4 ? KS * 64 : 256) void grouped_thin_kernel(Gr
 // A BM x BN tile by WR x WC waves.  The contraction goes through LDS in steps of 64, in five buffers that hold a step of one
 // operand each: while two are read, three are filled, the columns' operand two steps ahead and the rows' one and a half.  Pieces go
 // straight from memory into LDS.  An operand whose rows run along the contraction (`along`) lies in LDS row by row, 128 bytes
-// each, an operand whose rows run across it (`across`) step by step; the latter is turned by the transposing LDS read.
-// The 16-byte pieces of a row are permuted by the row's number, so that the rows (or steps)
-// that a read touches at once lie in different banks; as the loads write LDS in lane order it is the source address that is
-// permuted.
-__device__ uint4 zero_piece[1];
-
-
-// 16 bytes a lane from src to dst + 16 * lane, dst the same for the wave.  Written as an instruction of its own because the compiler
-// counts the builtin as an access that may return out of order and then waits for every LDS read at once; it returns nothing in a
-// register, and meet() waits for it.
-__device__ __forceinline__ void piece_to_lds(const void* src, void* dst) {
-  const uint32_t at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(LdsVoid*)dst);
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(at), "v"(src) : "memory");
-}
+// each, an operand whose rows run across it (`across`) step by step; the latter is turned by the transposing LDS read.  The
+// 16-byte pieces of a row are permuted by the row's number, so that the rows (or steps) that a read touches at once lie in
+// different banks; as the loads write LDS in lane order it is the source address that is permuted.
+//
+// Workgroups take one tile after the other: while the last two steps of a tile run, the first two of the next are fetched, and a
+// tile's results are stored while the next one's products run.  For that every tile has at least two steps, a gradient's three, as
+// the rows of x that a step takes are looked up a step before they are fetched; steps behind the contraction's end hold zeros.
 constexpr int kStep = 64;
+constexpr uint32_t kNowhere = 0xfffffff0u;  // an offset behind every buffer's end: reads as zeros
 
-// How the pieces of a row change places: of a row of the rows' operand by the 16-byte piece, of the columns' operand too, but in
-// the order in which its fragments take the rows; of step e of an `across` operand by 32 bytes.
+// How the pieces of a row change places: of row r (column c) of an `along` operand the 16-byte pieces, of step e of an `across`
+// operand the 32-byte pieces.  A read takes the 128 bytes of eight lanes and of the eight sixteen lanes further at once.
 __device__ __forceinline__ int row_shift(int r) { return r & 7; }
-__device__ __forceinline__ int col_shift(int c) { return ((c >> 3) & 3) | ((c << 1) & 4); }
+__device__ __forceinline__ int col_shift(int c) { return ((c >> 2) & 2) | ((c << 1) & 4) | ((c >> 4) & 1); }
 __device__ __forceinline__ int across_shift(int e) { return (e & 3) | ((e >> 1) & 4); }
 
 // Column (from the wave's first) of value i of column fragment b.  A lane gets values 4 q ... 4 q + 3 of every fragment (q = lane /
 // 16); so that those of two fragments are eight neighbours, one 16-byte store, the columns are dealt out in this order.
 __device__ __forceinline__ int fragment_col(int b, int i) { return (b >> 1) * 32 + (i >> 2) * 8 + (b & 1) * 4 + (i & 3); }
 
-template <typename T>
-__device__ __forceinline__ typename Matrix<T>::Chunk along_piece(const T* tile, int r, int shift, int piece) {
-  return *reinterpret_cast<const typename Matrix<T>::Chunk*>(tile + r * kStep + ((piece ^ shift) << 3));
+// A buffer of `bytes` bytes from p on, the same for the wave, for loads that read zeros behind its end.
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ i32x4 buffer_of(const void* p, uint32_t bytes) {
+  const uint64_t at = reinterpret_cast<uint64_t>(p);
+  return i32x4{__builtin_amdgcn_readfirstlane((int)at), __builtin_amdgcn_readfirstlane((int)((at >> 32) & 0xffff)),
+               __builtin_amdgcn_readfirstlane((int)bytes), 0x00027000};
 }
-// Values first + 0 ... 3 (this lane's part of the columns) of steps e and e + 4, turned.
-template <typename T, int EXT>
-__device__ __forceinline__ typename Matrix<T>::Chunk across_piece(const T* tile, int col, int e) {
-  union {
-    short4v part[2];
-    typename Matrix<T>::Chunk whole;
-  } u;
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const T* p = tile + (e + 4 * h) * EXT + (((col >> 4) ^ across_shift(e + 4 * h)) << 4) + (col & 15);
-    u.part[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsShort4*)p);
-  }
-  return u.whole;
+// 16 bytes a lane from `offset` + `step` of the buffer to dst + 16 * lane, dst and step the same for the wave.  An instruction of
+// its own, as before the transposing LDS reads the compiler waits for every load into LDS that it knows of; it returns nothing in
+// a register, and meet() waits for it.
+__device__ __forceinline__ void piece_to_lds(i32x4 buffer, uint32_t offset, uint32_t step, const char* dst) {
+  const uint32_t at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(LdsVoid*)dst);
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(at), "v"(offset), "s"(buffer),
+               "s"(__builtin_amdgcn_readfirstlane(step))
+               : "memory");
 }
 
-// Workgroups take one tile after the other: while the last two steps of a tile run, the first two of the next are fetched, and a
-// tile's results are stored while the next one's products run.  For that every tile has at least two steps, a gradient's three, as
-// the rows of x that a step takes are looked up a step before they are fetched; steps behind the contraction's end hold zeros.
+struct TileArgs {
+  const void *rmat, *cmat;
+  void* out;
+  const int32_t *offsets, *order;
+  int64_t ldr, ldc, ldg, ldo, ldog;
+  int64_t rows, xrows;
+  uint32_t rbytes, cbytes;  // of rmat; of cmat, for products of one group's matrix
+  int groups, slots, outr, outc, depth, row_tiles, col_tiles;
+  Parts parts;
+};
+
 template <typename T, int FORM, int BM, int BN, int WR, int WC>
-__global__ __launch_bounds__(WR * WC * 64) void grouped_tile_kernel(
-    const T* __restrict__ rmat, const T* __restrict__ cmat, T* __restrict__ out, const int32_t* __restrict__ offsets,
-    const int32_t* __restrict__ order, int64_t ldr, int64_t ldc, int64_t ldg, int64_t ldo, int64_t ldog, int64_t rows,
-    int64_t xrows, int groups, int slots, int outr, int outc, int depth, int row_tiles, int col_tiles, Parts parts) {
+__global__ __launch_bounds__(WR * WC * 64) void grouped_tile_kernel(TileArgs a) {
   typedef typename Matrix<T>::Chunk Chunk;
   typedef T Part __attribute__((ext_vector_type(8)));
   constexpr int NW = WR * WC;
@@ -436,12 +433,11 @@ __global__ __launch_bounds__(WR * WC * 64) void grouped_tile_kernel(
   constexpr bool R_ALONG = FORM != kGradient, C_ALONG = FORM == kProduct;
   constexpr int LR = BM / 8 / NW, LC = BN / 8 / NW;  // loads of 1 KB a wave and step
   static_assert(LR * 8 * NW == BM && LC * 8 * NW == BN && FR % 4 == 0 && FC % 2 == 0, "");
-  constexpr int BUFFERS = 5, BUFFER = (BM > BN ? BM : BN) * kStep;
-  __shared__ __attribute__((aligned(1024))) T lds[BUFFERS * BUFFER];
+  constexpr int BUFFERS = 5, BUFFER = (BM > BN ? BM : BN) * kStep * 2;  // bytes
+  __shared__ __attribute__((aligned(1024))) char lds[BUFFERS * BUFFER];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wr = wave / WC * (BM / WR), wc = wave % WC * (BN / WC);
-  const T* const zero = reinterpret_cast<const T*>(zero_piece);
 
   // ---- the tiles ----
   struct Tile {
@@ -449,31 +445,30 @@ __global__ __launch_bounds__(WR * WC * 64) void grouped_tile_kernel(
     int64_t pbegin;
     int length;
   };
-  const TileWalk<BM> walk(offsets, FORM == kGradient ? 0 : groups, rows, FORM == kGradient ? 1 : col_tiles);
-  const GroupOrder by_length(offsets, FORM == kGradient && !parts.part ? groups : 0, rows);
-  const PartList part_list(offsets, FORM == kGradient && parts.part ? groups : 0, rows, parts.part);
-  const int64_t group_parts = FORM != kGradient ? 0 : parts.part ? part_list.total : groups;
-  const int per_group = row_tiles * col_tiles;  // gradient
+  const TileWalk<BM> walk(a.offsets, FORM == kGradient ? 0 : a.groups, a.rows, FORM == kGradient ? 1 : a.col_tiles);
+  const GroupOrder by_length(a.offsets, FORM == kGradient && !a.parts.part ? a.groups : 0, a.rows);
+  const PartList part_list(a.offsets, FORM == kGradient && a.parts.part ? a.groups : 0, a.rows, a.parts.part);
+  const int per_group = a.row_tiles * a.col_tiles;  // gradient
+  const int64_t group_parts = FORM != kGradient ? 0 : a.parts.part ? part_list.total : a.groups;
   // A gradient's tiles take as long as their groups are.  From the longest group to the shortest they are dealt out to all
   // workgroups, to and fro.
-  const int64_t count =
-      FORM == kGradient ? (group_parts * per_group + gridDim.x - 1) / gridDim.x : walk.count;
+  const int64_t count = FORM == kGradient ? (group_parts * per_group + gridDim.x - 1) / gridDim.x : walk.count;
   auto tile_at = [&](int64_t i, Tile& t) {  // false: there is none (only the last one of a gradient)
     if (FORM == kGradient) {
       const int64_t at = i * gridDim.x + (i & 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
       if (at >= group_parts * per_group) return false;
       const int g = (int)(at / per_group), in = (int)(at - (int64_t)g * per_group);
-      t.r0 = in / col_tiles * BM;
-      t.c0 = in % col_tiles * BN;
-      t.rn = min(BM, outr - t.r0);
-      if (parts.part) {
+      t.r0 = in / a.col_tiles * BM;
+      t.c0 = in % a.col_tiles * BN;
+      t.rn = min(BM, a.outr - t.r0);
+      if (a.parts.part) {
         const RowTile r = part_list.at(g);
         t.group = g;  // the part's number: where its sums go
         t.pbegin = r.begin;
         t.length = r.count;
       } else {
         t.group = by_length.at(g);
-        const GroupRange r = group_range(offsets, groups, rows, t.group);
+        const GroupRange r = group_range(a.offsets, a.groups, a.rows, t.group);
         t.pbegin = r.begin;
         t.length = (int)(r.end - r.begin);
       }
@@ -484,134 +479,164 @@ __global__ __launch_bounds__(WR * WC * 64) void grouped_tile_kernel(
       t.rn = r.count;
       t.pbegin = r.begin;
       t.c0 = r.col * BN;
-      t.length = depth;
+      t.length = a.depth;
     }
-    t.cn = min(BN, outc - t.c0);
+    t.cn = min(BN, a.outc - t.c0);
     return true;
   };
 
   // ---- what a lane loads ----
-  // `along` a fixed row, `across` a fixed column of its operand, and one step after the other of it.  Rows and columns outside the
-  // tile take the last one's values, which nothing stores; steps beyond the contraction's end come from a piece of zeros.
-  const T *rp[LR], *cp[LC];
-  const int along_r = lane >> 3;  // row within the eight that a load brings
-  int re[LR], ce[LC];
-#pragma unroll
-  for (int u = 0; u < LR; ++u) re[u] = R_ALONG ? ((lane & 7) ^ row_shift(along_r)) * 8
-                                               : (wave * LR + u) * (512 / BM) + lane / (BM / 8);
-#pragma unroll
-  for (int u = 0; u < LC; ++u) ce[u] = C_ALONG ? ((lane & 7) ^ col_shift((wave * LC + u) * 8 + along_r)) * 8
-                                               : (wave * LC + u) * (512 / BN) + lane / (BN / 8);
+  // `along` a fixed row, `across` a fixed column of its operand, one step after the other: an offset in bytes that stays for the
+  // tile and one, the same for all, that goes on with the steps.  Rows and columns outside the tile take the last one's values,
+  // which nothing stores.
+  const i32x4 rres = buffer_of(a.rmat, a.rbytes);
+  i32x4 cres = buffer_of(a.cmat, a.cbytes);
+  const uint32_t rstep = R_ALONG ? kStep * 2 : (uint32_t)(kStep * 2 * a.ldr);
+  const uint32_t cstep = C_ALONG ? kStep * 2 : FORM == kTransposed ? (uint32_t)(kStep * 2 * a.ldc) : 0;
+  uint32_t ro[LR], co[LC], rat = 0, cat = 0;
+  // which step (`across`) or value (`along`) of the contraction load u brings, from the pointed-at step's first
+  auto row_e = [&](int u) {
+    return R_ALONG ? ((lane & 7) ^ row_shift(lane >> 3)) * 8 : (wave * LR + u) * (512 / BM) + lane / (BM / 8);
+  };
+  auto col_e = [&](int u) {
+    return C_ALONG ? ((lane & 7) ^ col_shift((wave * LC + u) * 8 + (lane >> 3))) * 8 : (wave * LC + u) * (512 / BN) + lane / (BN / 8);
+  };
   int32_t look[FORM == kGradient ? LC : LR];  // source rows: of the next tile, of the gradient's next step
   auto look_up_rows = [&](const Tile& t) {
     if (FORM != kGradient) {
 #pragma unroll
       for (int u = 0; u < LR; ++u)
-        look[u] = (int32_t)source_row(order, t.pbegin + min((wave * LR + u) * 8 + along_r, t.rn - 1), slots, xrows);
+        look[u] = (int32_t)source_row(a.order, t.pbegin + min((wave * LR + u) * 8 + (lane >> 3), t.rn - 1), a.slots, a.xrows);
     }
   };
   auto look_up_step = [&](int64_t pbegin, int rest) {  // a step from grouped row pbegin on, `rest` rows are left
     if (FORM == kGradient) {
 #pragma unroll
-      for (int u = 0; u < LC; ++u) look[u] = ce[u] < rest ? (int32_t)source_row(order, pbegin + ce[u], slots, xrows) : -1;
+      for (int u = 0; u < LC; ++u)
+        look[u] = col_e(u) < rest ? (int32_t)source_row(a.order, pbegin + col_e(u), a.slots, a.xrows) : -1;
     }
   };
   auto mask_rows = [&](int left) {  // the last step: what lies behind the end
 #pragma unroll
-    for (int u = 0; u < LR; ++u) rp[u] = re[u] < left ? rp[u] : zero;
+    for (int u = 0; u < LR; ++u) ro[u] = row_e(u) < left ? ro[u] : kNowhere;
   };
   auto mask_cols = [&](int left) {
 #pragma unroll
-    for (int u = 0; u < LC; ++u) cp[u] = ce[u] < left ? cp[u] : zero;
+    for (int u = 0; u < LC; ++u) co[u] = col_e(u) < left ? co[u] : kNowhere;
   };
   auto begin_rows = [&](const Tile& t) {
 #pragma unroll
     for (int u = 0; u < LR; ++u) {
       if (R_ALONG)
-        rp[u] = rmat + (look[u] < 0 ? 0 : look[u]) * ldr + re[u];
+        ro[u] = (uint32_t)((max(look[u], 0) * a.ldr + row_e(u)) * 2);
       else
-        rp[u] = rmat + (t.pbegin + re[u]) * ldr + t.r0 + min((lane % (BM / 8) ^ (across_shift(re[u]) << 1)) * 8, t.rn - 8);
+        ro[u] = (uint32_t)((row_e(u) * a.ldr + t.r0 + min((lane % (BM / 8) ^ (across_shift(row_e(u)) << 1)) * 8, t.rn - 8)) * 2);
     }
+    rat = R_ALONG ? 0 : (uint32_t)(t.pbegin * a.ldr * 2);
     if (t.length < kStep) mask_rows(t.length);
   };
-  auto col_of = [&](int c0, int cn, int u) { return c0 + min((lane % (BN / 8) ^ (across_shift(ce[u]) << 1)) * 8, cn - 8); };
+  auto col_of = [&](int c0, int cn, int u) { return c0 + min((lane % (BN / 8) ^ (across_shift(col_e(u)) << 1)) * 8, cn - 8); };
   auto step_cols = [&](int c0, int cn) {  // gradient: the rows that were looked up
 #pragma unroll
-    for (int u = 0; u < LC; ++u) cp[u] = look[u] < 0 ? zero : cmat + look[u] * ldc + col_of(c0, cn, u);
+    for (int u = 0; u < LC; ++u) co[u] = look[u] < 0 ? kNowhere : (uint32_t)((look[u] * a.ldc + col_of(c0, cn, u)) * 2);
   };
   auto begin_cols = [&](const Tile& t) {
     if (FORM == kGradient) {
       step_cols(t.c0, t.cn);
       return;
     }
-    const T* base = cmat + (int64_t)t.group * ldg;
+    cres = buffer_of(static_cast<const T*>(a.cmat) + (int64_t)t.group * a.ldg, a.cbytes);
+    cat = 0;
 #pragma unroll
     for (int u = 0; u < LC; ++u) {
       if (C_ALONG)
-        cp[u] = base + (int64_t)(t.c0 + min((wave * LC + u) * 8 + along_r, t.cn - 1)) * ldc + ce[u];
+        co[u] = (uint32_t)(((t.c0 + min((wave * LC + u) * 8 + (lane >> 3), t.cn - 1)) * a.ldc + col_e(u)) * 2);
       else
-        cp[u] = base + ce[u] * ldc + col_of(t.c0, t.cn, u);
+        co[u] = (uint32_t)((col_e(u) * a.ldc + col_of(t.c0, t.cn, u)) * 2);
     }
     if (t.length < kStep) mask_cols(t.length);
   };
-  auto fetch_row = [&](int u, int buffer) { piece_to_lds(rp[u], lds + buffer * BUFFER + (wave * LR + u) * 512); };
-  auto fetch_col = [&](int u, int buffer) { piece_to_lds(cp[u], lds + buffer * BUFFER + (wave * LC + u) * 512); };
+  auto fetch_row = [&](int u, int buffer) {
+    piece_to_lds(rres, ro[u], rat, lds + buffer + (wave * LR + u) * 1024);
+  };
+  auto fetch_col = [&](int u, int buffer) {
+    piece_to_lds(cres, co[u], cat, lds + buffer + (wave * LC + u) * 1024);
+  };
 
   f32x4 acc[FR][FC];
   auto clear = [&]() {
 #pragma unroll
-    for (int a = 0; a < FR; ++a)
+    for (int f = 0; f < FR; ++f)
 #pragma unroll
-      for (int b = 0; b < FC; ++b) acc[a][b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+      for (int b = 0; b < FC; ++b) acc[f][b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   };
-  int sub = lane & 15, quad = lane >> 4;
+  // ---- what a lane reads ----
+  // Offsets into a buffer, of which everything that is the same for the wave is left out: it goes into the instruction.
+  const int sub = lane & 15, quad = lane >> 4;
+  const int turn = quad * 8 + (sub >> 2);  // step of an `across` read
+  const int rlane = R_ALONG ? sub * 128 + ((quad ^ row_shift(sub)) << 4) : turn * (BM * 2) + (sub & 3) * 8 + wr * 2;
+  const int clane = C_ALONG ? fragment_col(0, sub) * 128 + ((quad ^ col_shift(fragment_col(0, sub))) << 4)
+                            : turn * (BN * 2) + (sub & 1) * 16 + wc * 2;
+  const int rturn = across_shift(turn) << 5, cturn = (across_shift(turn) ^ ((sub >> 1) & 1)) << 5;
+  auto turned = [&](const char* p, int pitch) {  // steps e and e + 4
+    union {
+      short4v part[2];
+      Chunk whole;
+    } u;
+    u.part[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsShort4*)p);
+    u.part[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsShort4*)(p + 4 * pitch));
+    return u.whole;
+  };
   auto col_fragments = [&](int buffer, int kk, Chunk (&f)[FC]) {
-    const T* tile = lds + buffer * BUFFER;
+    if (C_ALONG) {
+      const char* p = lds + (buffer + wc * 128) + (clane ^ (kk << 6));
 #pragma unroll
-    for (int b = 0; b < FC; ++b) {
-      if (C_ALONG) {
-        const int c = wc + fragment_col(b, sub);
-        f[b] = along_piece(tile, c, col_shift(c), kk * 4 + quad);
-      } else {
-        f[b] = across_piece<T, BN>(tile, wc + fragment_col(b, (sub & 3) * 4), kk * 32 + quad * 8 + (sub >> 2));
+      for (int b = 0; b < FC; ++b) f[b] = *reinterpret_cast<const Chunk*>(p + fragment_col(b, 0) * 128);
+    } else {
+#pragma unroll
+      for (int b = 0; b < FC; b += 2) {  // the pieces of 32 columns from wc + 16 b on: wc is whole eights of them but for bit 2
+        const char* p = lds + (buffer + kk * 32 * BN * 2 - (wc & 127) * 2) + clane + (cturn ^ ((((wc >> 4) & 7) + b) << 5));
+        f[b] = turned(p, BN * 2);
+        f[b + 1] = turned(p + 8, BN * 2);
       }
     }
   };
   auto row_fragments = [&](int buffer, int kk, int pair, Chunk (&f)[2]) {
-    const T* tile = lds + buffer * BUFFER;
+    if (R_ALONG) {
+      const char* p = lds + (buffer + wr * 128) + (rlane ^ (kk << 6));
 #pragma unroll
-    for (int a = 0; a < 2; ++a) {
-      const int r = wr + (pair * 2 + a) * 16;
-      if (R_ALONG)
-        f[a] = along_piece(tile, r + sub, row_shift(r + sub), kk * 4 + quad);
-      else
-        f[a] = across_piece<T, BM>(tile, r + (sub & 3) * 4, kk * 32 + quad * 8 + (sub >> 2));
+      for (int h = 0; h < 2; ++h) f[h] = *reinterpret_cast<const Chunk*>(p + (pair * 2 + h) * 2048);
+    } else {
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        f[h] = turned(lds + (buffer + kk * 32 * BM * 2 - (wr & 127) * 2) + rlane + (rturn ^ ((((wr >> 4) & 7) + pair * 2 + h) << 5)), BM * 2);
     }
   };
   auto multiply = [&](int pair, const Chunk (&fr)[2], const Chunk (&fc)[FC]) {
 #pragma unroll
-    for (int a = 0; a < 2; ++a)
+    for (int h = 0; h < 2; ++h)
 #pragma unroll
-      for (int b = 0; b < FC; ++b) acc[pair * 2 + a][b] = Matrix<T>::mma(fc[b], fr[a], acc[pair * 2 + a][b]);
+      for (int b = 0; b < FC; ++b) acc[pair * 2 + h][b] = Matrix<T>::mma(fc[b], fr[h], acc[pair * 2 + h][b]);
   };
   auto store = [&](const Tile& t) {
-    T* base = FORM == kGradient ? out + (int64_t)t.group * ldog + (int64_t)t.r0 * ldo : out + t.pbegin * ldo;
-    const int64_t known = xrows * slots;
+    T* out = static_cast<T*>(a.out);
+    T* base = FORM == kGradient ? out + (int64_t)t.group * a.ldog + (int64_t)t.r0 * a.ldo : out + t.pbegin * a.ldo;
+    const int64_t known = a.xrows * a.slots;
 #pragma unroll
-    for (int a = 0; a < FR; ++a) {
-      const int row = wr + a * 16 + sub;
+    for (int f = 0; f < FR; ++f) {
+      const int row = wr + f * 16 + sub;
       if (row >= t.rn) continue;
-      T* orow = base + row * ldo + t.c0;
-      if (FORM == kGradient && parts.part) {
-        float* sums = parts.sums + ((int64_t)t.group * outr + t.r0 + row) * outc + t.c0;
+      T* orow = base + row * a.ldo + t.c0;
+      if (FORM == kGradient && a.parts.part) {
+        float* sums = a.parts.sums + ((int64_t)t.group * a.outr + t.r0 + row) * a.outc + t.c0;
 #pragma unroll
         for (int b = 0; b < FC; ++b) {
           const int col = wc + fragment_col(b, quad * 4);
-          if (col < t.cn) *reinterpret_cast<f32x4*>(sums + col) = acc[a][b];
+          if (col < t.cn) *reinterpret_cast<f32x4*>(sums + col) = acc[f][b];
         }
         continue;
       }
-      const bool none = FORM != kGradient && order && (uint32_t)order[t.pbegin + row] >= known;  // a row of zeros
+      const bool none = FORM != kGradient && a.order && (uint32_t)a.order[t.pbegin + row] >= known;  // a row of zeros
 #pragma unroll
       for (int b = 0; b < FC; b += 2) {
         const int col = wc + fragment_col(b, quad * 4);
@@ -619,8 +644,8 @@ __global__ __launch_bounds__(WR * WC * 64) void grouped_tile_kernel(
           Part q;
 #pragma unroll
           for (int u = 0; u < 4; ++u) {
-            q[u] = static_cast<T>(none ? 0.0f : acc[a][b][u]);
-            q[u + 4] = static_cast<T>(none ? 0.0f : acc[a][b + 1][u]);
+            q[u] = static_cast<T>(none ? 0.0f : acc[f][b][u]);
+            q[u + 4] = static_cast<T>(none ? 0.0f : acc[f][b + 1][u]);
           }
           *reinterpret_cast<Part*>(orow + col) = q;
         }
@@ -644,7 +669,7 @@ __global__ __launch_bounds__(WR * WC * 64) void grouped_tile_kernel(
     constexpr int LEAST = FORM == kGradient ? 3 : 2;
     auto steps_of = [&](const Tile& t) { return max(LEAST, (t.length + kStep - 1) / kStep); };
     int left = steps_of(tile);                            // steps of this tile
-    int fleft = left, ftail = tile.length;                // steps and rest of the contraction where the pointers stand
+    int fleft = left, ftail = tile.length;                // steps and rest of the contraction where the loads stand
     int fc0 = tile.c0, fcn = tile.cn;                     // and its columns
     int64_t lbegin = tile.pbegin;                         // the same where rows are looked up, a step further
     int lleft = left, ltail = tile.length;
@@ -667,14 +692,9 @@ __global__ __launch_bounds__(WR * WC * 64) void grouped_tile_kernel(
     auto advance = [&]() {
       if (--fleft > 0) {
         ftail -= kStep;
-#pragma unroll
-        for (int u = 0; u < LR; ++u) rp[u] += R_ALONG ? (int64_t)kStep : kStep * ldr;
-        if (FORM == kGradient) {
-          step_cols(fc0, fcn);
-        } else {
-#pragma unroll
-          for (int u = 0; u < LC; ++u) cp[u] += C_ALONG ? (int64_t)kStep : kStep * ldc;
-        }
+        rat += rstep;
+        cat += cstep;
+        if (FORM == kGradient) step_cols(fc0, fcn);
         if (ftail < kStep) {
           mask_rows(ftail);
           if (FORM != kGradient) mask_cols(ftail);
@@ -695,7 +715,7 @@ __global__ __launch_bounds__(WR * WC * 64) void grouped_tile_kernel(
       more = index + 1 < count && tile_at(index + 1, next);
       if (more) look_up_rows(next);
     };
-    int cnow = 0, rnow = 1, cnext = 2, rnext = 3, ahead = 4;  // buffers of this step, of the next one, and the free one
+    int cnow = 0, rnow = BUFFER, cnext = 2 * BUFFER, rnext = 3 * BUFFER, ahead = 4 * BUFFER;  // this step, the next one, free
     look_up_rows(tile);
     look_up_step(lbegin, ltail);
     begin_rows(tile);
@@ -714,7 +734,6 @@ __global__ __launch_bounds__(WR * WC * 64) void grouped_tile_kernel(
     col_fragments(cnow, 0, fc[0]);
     row_fragments(rnow, 0, 0, fr[0]);
     for (;;) {
-      asm volatile("" : "+v"(sub), "+v"(quad));  // LDS addresses are made anew in every step: there are no registers to keep them
 #pragma unroll
       for (int p = 0; p < PAIRS; ++p) {
         __builtin_amdgcn_sched_barrier(0);
@@ -776,14 +795,14 @@ __global__ __launch_bounds__(WR * WC * 64) void grouped_tile_kernel(
   }
 
   if (FORM != kGradient) {  // rows behind the last group
-    const GroupRange g = group_range(offsets, groups, rows, groups);
-    const int parts = outc / 8;
-    const int64_t count = (g.end - g.begin) * parts;
+    const GroupRange g = group_range(a.offsets, a.groups, a.rows, a.groups);
+    const int parts = a.outc / 8;
+    const int64_t pieces = (g.end - g.begin) * parts;
     Part q;
 #pragma unroll
     for (int u = 0; u < 8; ++u) q[u] = static_cast<T>(0.0f);
-    for (int64_t i = (int64_t)blockIdx.x * (NW * 64) + tid; i < count; i += (int64_t)gridDim.x * (NW * 64))
-      *reinterpret_cast<Part*>(out + (g.begin + i / parts) * ldo + i % parts * 8) = q;
+    for (int64_t i = (int64_t)blockIdx.x * (NW * 64) + tid; i < pieces; i += (int64_t)gridDim.x * (NW * 64))
+      *reinterpret_cast<Part*>(static_cast<T*>(a.out) + (g.begin + i / parts) * a.ldo + i % parts * 8) = q;
   }
 }
 
@@ -818,6 +837,9 @@ hipError_t thin_typed(const GroupedArgs& a, hipStream_t st) {
   return hipGetLastError();
 }
 
+// Offsets in bytes of 16-bit values, a step of 64 rows beyond the last included, fit 32 bits.
+bool short_offsets(int64_t rows, int64_t ld) { return rows > 0 && (rows + 3 * kStep) * ld * 2 < (int64_t)0xf0000000; }
+
 // Tiles of a general kernel: 128 x 128 where there are enough of them, else 64 x 64.
 bool large_tiles(int64_t row_tiles_128, int64_t cols, int row_parts = 1) { return row_tiles_128 * ((cols + 127) / 128) * row_parts >= 512; }
 
@@ -838,7 +860,8 @@ hipError_t product_typed(const GroupedArgs& a, bool transpose, hipStream_t st) {
   constexpr int CH = Matrix<T>::kChunk;
   const int outc = transpose ? a.K : a.N, depth = transpose ? a.N : a.K;
   const bool tiled = sizeof(T) == 2 && whole_chunks<T>(a.x, a.ldx) && whole_chunks<T>(a.w, a.ldw) && a.ldg % CH == 0 &&
-                     a.K % CH == 0 && a.N % CH == 0 && whole_chunks<T>(a.y, a.ldy);
+                     a.K % CH == 0 && a.N % CH == 0 && whole_chunks<T>(a.y, a.ldy) && short_offsets(a.xrows, a.ldx) &&
+                     short_offsets(a.N, a.ldw);
   if (!transpose) {
     // Up to 8 rows a group the matrices are what takes time, and the kernel for few rows reads them as fast as any (64 groups of
     // 1024 x 2048 in 16 bits, 64 rows 53 us, tiles 57; 512 rows 73 and 72; in 32 bits 72, tiles of 64 x 64 91).  Beyond, tiles read
@@ -852,20 +875,15 @@ hipError_t product_typed(const GroupedArgs& a, bool transpose, hipStream_t st) {
   }
   if constexpr (sizeof(T) == 2) {
     if (tiled) {
-      constexpr int BM = 256, BN = 256;
-      const T *x = static_cast<const T*>(a.x), *w = static_cast<const T*>(a.w);
-      T* y = static_cast<T*>(a.y);
-      const int wcols = (outc + BN - 1) / BN;
-      const int64_t n = tile_bound(a.rows, a.groups, BM, wcols);
-      const uint32_t grid = (uint32_t)(n < 256 ? n : 256);
+      const int cols = (outc + 255) / 256;
+      const int64_t n = tile_bound(a.rows, a.groups, 256, cols);
+      const TileArgs t{a.x, a.w, a.y, a.offsets, a.order, a.ldx, a.ldw, a.ldg, a.ldy, 0, a.rows, a.xrows,
+                       (uint32_t)(((a.xrows - 1) * a.ldx + depth) * 2), (uint32_t)(((a.N - 1) * a.ldw + a.K) * 2),
+                       a.groups, a.slots, 0, outc, depth, 0, cols, Parts{0, nullptr}};
       if (transpose)
-        grouped_tile_kernel<T, kTransposed, BM, BN, 2, 4><<<grid, 512, 0, st>>>(
-            x, w, y, a.offsets, a.order, a.ldx, a.ldw, a.ldg, a.ldy, 0, a.rows, a.xrows, a.groups, a.slots, 0, outc, depth, 0, wcols,
-            Parts{0, nullptr});
+        grouped_tile_kernel<T, kTransposed, 256, 256, 2, 4><<<(uint32_t)(n < 256 ? n : 256), 512, 0, st>>>(t);
       else
-        grouped_tile_kernel<T, kProduct, BM, BN, 2, 4><<<grid, 512, 0, st>>>(
-            x, w, y, a.offsets, a.order, a.ldx, a.ldw, a.ldg, a.ldy, 0, a.rows, a.xrows, a.groups, a.slots, 0, outc, depth, 0, wcols,
-            Parts{0, nullptr});
+        grouped_tile_kernel<T, kProduct, 256, 256, 2, 4><<<(uint32_t)(n < 256 ? n : 256), 512, 0, st>>>(t);
       return hipGetLastError();
     }
   }
@@ -898,7 +916,7 @@ GradientCut gradient_cut(int64_t rows, int groups, int N, int K, int dtype) {
   const int64_t want = c.side == 256 ? 256 : c.side == 128 ? 1024 : 2048;  // workgroups
   c.part = 0;
   c.parts = 0;
-  if (groups * c.tiles < want && rows > 256) {
+  if (groups * c.tiles * 2 <= want && rows > 256) {
     int64_t part = rows * c.tiles / want;
     part = part < 128 ? 128 : (part + 63) / 64 * 64;
     if (part < rows) {
@@ -928,16 +946,18 @@ hipError_t gradient_typed(const GradientArgs& a, hipStream_t st) {
   if (c.part && !a.work) c.part = 0;
   const Parts parts{c.part, c.part ? static_cast<float*>(a.work) : nullptr};
   const bool tiled = sizeof(T) == 2 && whole_chunks<T>(a.x, a.ldx) && whole_chunks<T>(a.dy, a.lddy) && a.K % CH == 0 &&
-                     a.N % CH == 0 && whole_chunks<T>(a.dw, a.ldw) && a.ldg % CH == 0;
+                     a.N % CH == 0 && whole_chunks<T>(a.dw, a.ldw) && a.ldg % CH == 0 && short_offsets(a.rows, a.lddy) &&
+                     short_offsets(a.xrows, a.ldx);
   hipError_t e = hipSuccess;
   bool done = false;
   if constexpr (sizeof(T) == 2) {
     if (tiled && c.side == 256) {
       const int wr = (a.N + 255) / 256, wc = (a.K + 255) / 256;
       const int64_t n = (c.part ? c.parts : a.groups) * wr * wc;
-      grouped_tile_kernel<T, kGradient, 256, 256, 2, 4><<<(uint32_t)(n < 256 ? n : 256), 512, 0, st>>>(
-          static_cast<const T*>(a.dy), static_cast<const T*>(a.x), static_cast<T*>(a.dw), a.offsets, a.order, a.lddy, a.ldx, 0, a.ldw,
-          a.ldg, a.rows, a.xrows, a.groups, a.slots, a.N, a.K, 0, wr, wc, parts);
+      const TileArgs t{a.dy, a.x, a.dw, a.offsets, a.order, a.lddy, a.ldx, 0, a.ldw, a.ldg, a.rows, a.xrows,
+                       (uint32_t)(((a.rows - 1) * a.lddy + a.N) * 2), (uint32_t)(((a.xrows - 1) * a.ldx + a.K) * 2),
+                       a.groups, a.slots, a.N, a.K, 0, wr, wc, parts};
+      grouped_tile_kernel<T, kGradient, 256, 256, 2, 4><<<(uint32_t)(n < 256 ? n : 256), 512, 0, st>>>(t);
       e = hipGetLastError();
       done = true;
     }
