@@ -1,0 +1,122 @@
+"""A linear model per cluster, fed by a soft assignment: what a program does with the clusters that k-means found.
+
+    python -m paper_1802_04450_amd.cluster_experts
+
+makes points whose targets follow another linear map in every cluster, finds the clusters (``sc_kmeans``), trains the models and
+the centres with the operators of the library, and serves the trained models from 16 and from 8 bits.
+
+A row x has the scores -|x - c_j|^2 / (2 width^2) against the centres; its ``t`` best clusters (``sc_route``) each apply their
+matrix to ((x - c) / width, 1), c the best cluster's centre (``sc_grouped_product``), and the results are added up with the
+assignment's weights (``sc_group_combine``).
+"""
+from __future__ import annotations
+
+from typing import NamedTuple
+
+import torch
+
+from . import binding as sc
+
+
+class Saved(NamedTuple):
+    """What the backward pass needs of a forward pass."""
+    x: torch.Tensor
+    rows: torch.Tensor
+    scores: torch.Tensor
+    idx: torch.Tensor
+    weight: torch.Tensor
+    offsets: torch.Tensor
+    order: torch.Tensor
+    place: torch.Tensor
+    z: torch.Tensor
+
+
+class ClusterExperts:
+    """Centres (k, d) in fp32, matrices (k, out, d + 1 filled up to a multiple of 8) in fp32 with a copy in `dtype` for the
+    products."""
+
+    def __init__(self, centres: torch.Tensor, out: int, t: int = 2, width: float = 1.0, dtype: torch.dtype = torch.bfloat16):
+        k, d = centres.shape
+        self.t, self.width, self.dtype, self.d = t, width, dtype, d
+        self.centres = centres.float().clone()
+        self.weights = torch.zeros(k, out, (d + 1 + 7) // 8 * 8, device=centres.device)
+        self._eight = None
+
+    def _rows(self, x: torch.Tensor, idx: torch.Tensor) -> torch.Tensor:
+        rows = torch.zeros(x.shape[0], self.weights.shape[2], dtype=self.dtype, device=x.device)
+        rows[:, :self.d] = (x - self.centres[idx[:, 0].long()]) / self.width
+        rows[:, self.d] = 1.0
+        return rows
+
+    def _assign(self, x: torch.Tensor):
+        c = self.centres
+        far = (x * x).sum(1, keepdim=True) - 2.0 * (x @ c.t()) + (c * c).sum(1)
+        scores = far / (-2.0 * self.width ** 2)
+        return (scores, *sc.sc_route(scores, self.t))
+
+    def forward(self, x: torch.Tensor):
+        """x (n, d) fp32.  Returns the outputs (n, out) of `dtype` and what `backward` needs."""
+        scores, idx, weight, offsets, order, place = self._assign(x)
+        rows = self._rows(x, idx)
+        z = sc.sc_grouped_product(rows, self.weights.to(self.dtype), offsets, order=order, slots=self.t)
+        return sc.sc_group_combine(z, place, weight), Saved(x, rows, scores, idx, weight, offsets, order, place, z)
+
+    def backward(self, dout: torch.Tensor, s: Saved):
+        """Gradients of the matrices, and of the centres by way of the assignment, from that of the outputs."""
+        dz, dweight = sc.sc_group_combine_backward(dout, s.z, s.place, s.weight, s.order)
+        dweights = sc.sc_grouped_gradient(dz, s.rows, s.offsets, order=s.order, slots=self.t)
+        dscores = sc.sc_route_backward(s.scores, s.idx, s.weight, dweight)
+        # the score of row i and cluster j has the gradient (x_i - c_j) / width^2 in c_j
+        dcentres = (dscores.t() @ s.x - dscores.sum(0)[:, None] * self.centres) / self.width ** 2
+        return dweights, dcentres
+
+    def step(self, x: torch.Tensor, y: torch.Tensor, rate: float, centre_rate: float) -> torch.Tensor:
+        """One step of gradient descent on the mean squared error.  Returns the error before it.  A matrix's gradient is divided by
+        the rows that its cluster got, so that small clusters learn as quickly as large ones."""
+        out, saved = self.forward(x)
+        diff = out.float() - y
+        dweights, dcentres = self.backward(diff.to(self.dtype), saved)
+        got = (saved.offsets[1:] - saved.offsets[:-1]).clamp(min=1).float()
+        self.weights -= rate * dweights.float() / got[:, None, None]
+        self.centres -= centre_rate * dcentres / got[:, None]
+        self._eight = None
+        return (diff * diff).mean()
+
+    def serve8(self, x: torch.Tensor) -> torch.Tensor:
+        """The outputs with the matrices, and the rows, in 8 bits."""
+        if self._eight is None:
+            self._eight = sc.sc_quantize_blocks(self.weights)
+        _, idx, weight, offsets, order, place = self._assign(x)
+        q, scale = sc.sc_quantize_blocks(self._rows(x, idx))
+        z = sc.sc_grouped_product_e4m3(q, scale, *self._eight, offsets, order=order, slots=self.t, dtype=self.dtype)
+        return sc.sc_group_combine(z, place, weight)
+
+
+def example(n: int = 20_000, d: int = 16, k: int = 8, out: int = 12, steps: int = 60, seed: int = 0):
+    """Trains on points of k clusters with another linear map in each.  Returns (errors before every step, mean square of the
+    targets, outputs from 16 bits, outputs from 8 bits, targets)."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    normal = lambda *shape: torch.randn(*shape, generator=g, device="cuda")
+    true_centres, maps, shifts = 6.0 * normal(k, d), normal(k, out, d) / d ** 0.5, normal(k, out)
+    label = torch.randint(0, k, (n,), generator=g, device="cuda")
+    x = true_centres[label] + normal(n, d)
+    # every cluster's map acts on the distance from its centre
+    y = torch.matmul(maps[label], (x - true_centres[label])[:, :, None])[:, :, 0] + shifts[label]
+    _, centres, _, _ = sc.sc_kmeans(x.double(), k, seed, 50)
+    model = ClusterExperts(centres, out, t=2)
+    errors = [float(model.step(x, y, 0.4, 1e-2)) for _ in range(steps)]
+    return errors, float((y * y).mean()), model.forward(x)[0], model.serve8(x), y
+
+
+def main() -> None:
+    errors, size, out16, out8, y = example()
+    print(f"mean square of the targets {size:.3g}, error before step 1 {errors[0]:.3g}, 10 {errors[9]:.3g}, "
+          f"{len(errors)} {errors[-1]:.3g}")
+    gap = float((out16.float() - out8.float()).norm() / out16.float().norm())
+    print(f"error from 16 bits {float(((out16.float() - y) ** 2).mean()):.3g}, from 8 bits "
+          f"{float(((out8.float() - y) ** 2).mean()):.3g}, their outputs differ by {gap:.3f} of their size")
+
+
+if __name__ == "__main__":
+    main()

@@ -235,101 +235,139 @@ __global__ __launch_bounds__(256) void e4m3_any_kernel(E4m3Args a, int cols) {
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-// 8 numbers as bf16
-__device__ __forceinline__ bf16x8 widen(uint32_t lo, uint32_t hi) {
-  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, true);
-  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, true);
+// 8 numbers times the power of two that a scale byte stands for, as bf16.  The conversion takes the power from the exponent bits of
+// a float, which is what the byte is.
+__device__ __forceinline__ bf16x8 widen(uint32_t lo, uint32_t hi, int scale) {
+  const float s = __uint_as_float((uint32_t)scale << 23);
+  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, s, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, s, true);
+  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, s, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, s, true);
   return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
-// The same tile with the factors as bf16 in LDS.
-constexpr int kWidePitch = kScaleBlock + 8;
+// Powers of two whose numbers bf16 holds all: 2^-9 of 2^-111 up to 448 of 2^119.  Where a block has another one, the numbers go without
+// theirs, and the sums over that part of the contraction are multiplied afterwards.
+__device__ __forceinline__ bool held(int scale) { return scale >= 16 && scale <= 246; }
+__device__ __forceinline__ float times_scales(float v, int s, int t) { return s == 255 || t == 255 ? NAN : ldexpf(v, s + t - 254); }
 
-__global__ __launch_bounds__(256) void e4m3_wide_kernel(E4m3Args a, int cols) {
-  __shared__ __attribute__((aligned(16))) __bf16 xt[kTile * kWidePitch], wt[kTile * kWidePitch];
-  const RowTile t = find_tile<kTile>(a.offsets, a.groups, a.rows, cols);
+// A TILE x TILE tile by four waves, a quarter each, with the factors as bf16 in two buffers of LDS, 64 values of every row at a
+// time: the next ones are loaded while this step's products run.
+template <int TILE>
+__global__ __launch_bounds__(256, 2) void e4m3_wide_kernel(E4m3Args a, int cols) {
+  constexpr int STEP = 64, PITCH = STEP + 8, LOADS = TILE * (STEP / 16) / 256, F = TILE / 32;
+  __shared__ __attribute__((aligned(16))) __bf16 lds[2][2][TILE * PITCH];
+  __shared__ uint8_t scales[2][TILE];
+  const RowTile t = find_tile<TILE>(a.offsets, a.groups, a.rows, cols);
   if (t.group < 0) return;
   const bool empty = t.group == a.groups;
-  const int c0 = t.col * kTile, cn = min(kTile, a.N - c0);
+  const int c0 = t.col * TILE, cn = min(TILE, a.N - c0);
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-  const int wr = (wave >> 1) * 32, wc = (wave & 1) * 32;
-  const uint8_t *xp[2], *wp[2];
+  const int sub = lane & 15, quad = lane >> 4;
+  const int wr = (wave >> 1) * (TILE / 2), wc = (wave & 1) * (TILE / 2);
+  // 16 numbers of row tid / 4 (+ 64) of each factor
+  const uint8_t *xp[LOADS], *wp[LOADS], *xsp[LOADS], *wsp[LOADS];
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const int r = (tid >> 3) + h * 32;
+  for (int u = 0; u < LOADS; ++u) {
+    const int r = (tid >> 2) + u * 64;
     const int64_t src = !empty && r < t.count ? source_row(a.order, t.begin + r, a.slots, a.xrows) : -1;
-    xp[h] = src < 0 ? nullptr : a.x + src * a.ldx + (tid & 7) * 16;
-    wp[h] = !empty && r < cn ? a.w + (int64_t)t.group * a.ldg + (int64_t)(c0 + r) * a.ldw + (tid & 7) * 16 : nullptr;
+    xp[u] = src < 0 ? nullptr : a.x + src * a.ldx + (tid & 3) * 16;
+    xsp[u] = src < 0 ? nullptr : a.xs + src * a.ldxs;
+    const bool there = !empty && r < cn;
+    wp[u] = there ? a.w + (int64_t)t.group * a.ldg + (int64_t)(c0 + r) * a.ldw + (tid & 3) * 16 : nullptr;
+    wsp[u] = there ? a.ws + (int64_t)t.group * a.ldgs + (int64_t)(c0 + r) * a.ldws : nullptr;
   }
-  // the scales of the results that the lane gets: two rows, twice four columns
-  const uint8_t *xsp[2], *wsp[2][4];
+  uint4 x[LOADS], w[LOADS];
+  int xs[LOADS], ws[LOADS];
+  auto load = [&](int step) {
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const int r = wr + h * 16 + (lane & 15), c = wc + h * 16 + (lane >> 4) * 4;
-    const int64_t src = !empty && r < t.count ? source_row(a.order, t.begin + r, a.slots, a.xrows) : -1;
-    xsp[h] = src < 0 ? nullptr : a.xs + src * a.ldxs;
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      wsp[h][i] = !empty && c + i < cn ? a.ws + (int64_t)t.group * a.ldgs + (int64_t)(c0 + c + i) * a.ldws : nullptr;
-  }
-  f32x4 acc[2][2];
-#pragma unroll
-  for (int u = 0; u < 2; ++u)
-#pragma unroll
-    for (int v = 0; v < 2; ++v) acc[u][v] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  const int steps = empty ? 0 : a.Kp / kScaleBlock;
-  for (int b = 0; b < steps; ++b) {
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int at = ((tid >> 3) + h * 32) * kWidePitch + (tid & 7) * 16;
-      const uint4 x = xp[h] ? *reinterpret_cast<const uint4*>(xp[h] + b * kScaleBlock) : make_uint4(0, 0, 0, 0);
-      const uint4 w = wp[h] ? *reinterpret_cast<const uint4*>(wp[h] + b * kScaleBlock) : make_uint4(0, 0, 0, 0);
-      *reinterpret_cast<bf16x8*>(xt + at) = widen(x.x, x.y);
-      *reinterpret_cast<bf16x8*>(xt + at + 8) = widen(x.z, x.w);
-      *reinterpret_cast<bf16x8*>(wt + at) = widen(w.x, w.y);
-      *reinterpret_cast<bf16x8*>(wt + at + 8) = widen(w.z, w.w);
+    for (int u = 0; u < LOADS; ++u) {
+      x[u] = w[u] = make_uint4(0, 0, 0, 0);
+      xs[u] = ws[u] = 127;
+      if (xp[u]) {
+        x[u] = *reinterpret_cast<const uint4*>(xp[u] + step * STEP);
+        xs[u] = xsp[u][step / 2];
+      }
+      if (wp[u]) {
+        w[u] = *reinterpret_cast<const uint4*>(wp[u] + step * STEP);
+        ws[u] = wsp[u][step / 2];
+      }
     }
-    __syncthreads();
-    f32x4 part[2][2];
+  };
+  f32x4 acc[F][F];
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
+  for (int u = 0; u < F; ++u)
 #pragma unroll
-      for (int v = 0; v < 2; ++v) part[u][v] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int v = 0; v < F; ++v) acc[u][v] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  const int steps = empty ? 0 : a.Kp / STEP;
+  if (steps > 0) load(0);
+  for (int s = 0; s < steps; ++s) {
+    __bf16 *xt = lds[s & 1][0], *wt = lds[s & 1][1];
+    auto put = [&](bool scaled) {
 #pragma unroll
-    for (int e = 0; e < kScaleBlock; e += 32) {
-      bf16x8 fx[2], fw[2];
+      for (int u = 0; u < LOADS; ++u) {
+        const int at = ((tid >> 2) + u * 64) * PITCH + (tid & 3) * 16;
+        const int sx = scaled ? xs[u] : 127, sw = scaled ? ws[u] : 127;
+        *reinterpret_cast<bf16x8*>(xt + at) = widen(x[u].x, x[u].y, sx);
+        *reinterpret_cast<bf16x8*>(xt + at + 8) = widen(x[u].z, x[u].w, sx);
+        *reinterpret_cast<bf16x8*>(wt + at) = widen(w[u].x, w[u].y, sw);
+        *reinterpret_cast<bf16x8*>(wt + at + 8) = widen(w[u].z, w[u].w, sw);
+      }
+    };
+    put(true);
+    bool all = true;
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        fx[h] = *reinterpret_cast<const bf16x8*>(xt + (wr + h * 16 + (lane & 15)) * kWidePitch + e + (lane >> 4) * 8);
-        fw[h] = *reinterpret_cast<const bf16x8*>(wt + (wc + h * 16 + (lane & 15)) * kWidePitch + e + (lane >> 4) * 8);
+    for (int u = 0; u < LOADS; ++u) all = all && held(xs[u]) && held(ws[u]);
+    if (__syncthreads_or(!all)) {  // the other buffer has been read by all by then
+      put(false);
+#pragma unroll
+      for (int u = 0; u < LOADS; ++u) {
+        scales[0][(tid >> 2) + u * 64] = (uint8_t)xs[u];
+        scales[1][(tid >> 2) + u * 64] = (uint8_t)ws[u];
+      }
+      __syncthreads();
+#pragma unroll 1
+      for (int u = 0; u < F; ++u)
+#pragma unroll 1
+        for (int v = 0; v < F; ++v) {
+          f32x4 part = {0.0f, 0.0f, 0.0f, 0.0f};
+          for (int e = 0; e < STEP; e += 32)
+            part = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                *reinterpret_cast<const bf16x8*>(wt + (wc + v * 16 + sub) * PITCH + e + quad * 8),
+                *reinterpret_cast<const bf16x8*>(xt + (wr + u * 16 + sub) * PITCH + e + quad * 8), part, 0, 0, 0);
+#pragma unroll
+          for (int f = 0; f < F * F; ++f)  // registers have no index
+            if (f == u * F + v)
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+                acc[f / F][f % F][i] += times_scales(part[i], scales[0][wr + u * 16 + sub], scales[1][wc + v * 16 + quad * 4 + i]);
+        }
+      __syncthreads();  // the scales have been read
+      if (s + 1 < steps) load(s + 1);
+      continue;
+    }
+    if (s + 1 < steps) load(s + 1);
+#pragma unroll
+    for (int e = 0; e < STEP; e += 32) {
+      bf16x8 fx[F], fw[F];
+#pragma unroll
+      for (int h = 0; h < F; ++h) {
+        fx[h] = *reinterpret_cast<const bf16x8*>(xt + (wr + h * 16 + sub) * PITCH + e + quad * 8);
+        fw[h] = *reinterpret_cast<const bf16x8*>(wt + (wc + h * 16 + sub) * PITCH + e + quad * 8);
       }
 #pragma unroll
-      for (int u = 0; u < 2; ++u)
+      for (int u = 0; u < F; ++u)
 #pragma unroll
-        for (int v = 0; v < 2; ++v) part[u][v] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fw[v], fx[u], part[u][v], 0, 0, 0);
+        for (int v = 0; v < F; ++v) acc[u][v] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fw[v], fx[u], acc[u][v], 0, 0, 0);
     }
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const int sx = xsp[u] ? xsp[u][b] : 127;
-#pragma unroll
-      for (int v = 0; v < 2; ++v)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int sw = wsp[v][i] ? wsp[v][i][b] : 127;
-          acc[u][v][i] += sx == 255 || sw == 255 ? NAN : ldexpf(part[u][v][i], sx + sw - 254);
-        }
-    }
-    __syncthreads();
   }
   float* y = static_cast<float*>(a.y);
 #pragma unroll
-  for (int u = 0; u < 2; ++u) {
-    const int row = wr + u * 16 + (lane & 15);
+  for (int u = 0; u < F; ++u) {
+    const int row = wr + u * 16 + sub;
     if (row >= t.count) continue;
     float* out = y + (t.begin + row) * a.ldy + c0;
 #pragma unroll
-    for (int v = 0; v < 2; ++v) {
-      const int col = wc + v * 16 + (lane >> 4) * 4;
+    for (int v = 0; v < F; ++v) {
+      const int col = wc + v * 16 + quad * 4;
 #pragma unroll
       for (int i = 0; i < 4; ++i)
         if (col + i < cn) out[col + i] = acc[u][v][i];
@@ -416,18 +454,20 @@ __global__ __launch_bounds__(KS > 4 ? KS * 64 : 256) void e4m3_thin_kernel(E4m3A
             const i32x8 q = __builtin_shufflevector(f[u][0], f[u][1], 0, 1, 2, 3, 4, 5, 6, 7);
             acc[r] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(p, q, acc[r], 0, 0, 0, sw[u], 0, sx[u]);
           } else {
-            f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
+            const bool all = !__any(!held(sw[u]) || !held(sx[u]));
+            const int tw = all ? sw[u] : 127, tx = all ? sx[u] : 127;
+            f32x4 sum = all ? acc[r] : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
               for (int e = 0; e < 4; e += 2)
-                sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen(now[u][h][e], now[u][h][e + 1]), widen(f[u][h][e], f[u][h][e + 1]),
-                                                              sum, 0, 0, 0);
-            // the lane's four results are of columns 4 quad ... 4 quad + 3, whose powers of two lie in those lanes
+                sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen(now[u][h][e], now[u][h][e + 1], tw),
+                                                              widen(f[u][h][e], f[u][h][e + 1], tx), sum, 0, 0, 0);
+            if (all) {
+              acc[r] = sum;
+            } else {  // the lane's four results are of columns 4 quad ... 4 quad + 3, whose powers of two lie in those lanes
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const int s = __shfl(sw[u], quad * 4 + i);
-              acc[r][i] += s == 255 || sx[u] == 255 ? NAN : ldexpf(sum[i], s + sx[u] - 254);
+              for (int i = 0; i < 4; ++i) acc[r][i] += times_scales(sum[i], __shfl(sw[u], quad * 4 + i), sx[u]);
             }
           }
         }
@@ -473,7 +513,10 @@ __global__ __launch_bounds__(KS > 4 ? KS * 64 : 256) void e4m3_thin_kernel(E4m3A
 // row hands over the same power of two.  Those come four steps at a time as one word a row, shifted by a byte a step.
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
-__device__ __forceinline__ int piece_shift(int r) { return (r >> 1) & 7; }
+// How the 16-byte pieces of row r (column c) change places: a read takes 128 bytes of eight lanes and of the eight sixteen lanes
+// further at once, which then lie in different banks.
+__device__ __forceinline__ int row_shift(int r) { return (r & 6) | ((r >> 4) & 1); }
+__device__ __forceinline__ int col_shift(int c) { return (c & 2) | ((c >> 1) & 4) | ((c >> 4) & 1); }
 // Column of value i of a column fragment: bits 2 and 3 change places, so that a lane's eight values of two neighbouring groups of
 // four are eight neighbours.
 __device__ __forceinline__ int fragment_col(int i) { return (i & 0x13) | ((i & 4) << 1) | ((i & 8) >> 1); }
@@ -510,8 +553,9 @@ __global__ __launch_bounds__(512) void e4m3_tile_kernel(E4m3Args a, int col_tile
   uint32_t ro[LOADS], co[LOADS];
   const int eight = lane >> 3;
   int32_t look[LOADS], looks[FR];  // source rows of the next tile: that the lane loads, whose scales it needs
-  const uint8_t *xsp[FR], *wsp[FC];
-  int sub = lane & 31, half = lane >> 5;
+  uint32_t xso[FR], wso[FC];  // where the scales of the lane's rows and columns begin
+  const uint8_t* wsbase = a.ws;
+  const int sub = lane & 31, half = lane >> 5;
   auto look_up = [&](const Tile& t) {
 #pragma unroll
     for (int u = 0; u < LOADS; ++u)
@@ -524,28 +568,30 @@ __global__ __launch_bounds__(512) void e4m3_tile_kernel(E4m3Args a, int col_tile
 #pragma unroll
     for (int u = 0; u < LOADS; ++u) {
       const int r = (wave * LOADS + u) * 8 + eight;
-      const int piece = ((lane & 7) ^ piece_shift(r)) * 16;
-      ro[u] = (uint32_t)(max(look[u], 0) * a.ldx + piece);
-      co[u] = (uint32_t)((int64_t)(t.c0 + min(r, t.cn - 1)) * a.ldw + piece);
+      ro[u] = (uint32_t)(max(look[u], 0) * a.ldx + ((lane & 7) ^ row_shift(r)) * 16);
+      co[u] = (uint32_t)((int64_t)(t.c0 + min(r, t.cn - 1)) * a.ldw + ((lane & 7) ^ col_shift(r)) * 16);
     }
     wres = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(a.w) + (int64_t)t.group * a.ldg, 0,
                                              (int)(uint32_t)((int64_t)(a.N - 1) * a.ldw + a.Kp), 0x00027000);
   };
   auto begin_scales = [&](const Tile& t) {
 #pragma unroll
-    for (int f = 0; f < FR; ++f) xsp[f] = a.xs + max(looks[f], 0) * a.ldxs;
+    for (int f = 0; f < FR; ++f) xso[f] = (uint32_t)(max(looks[f], 0) * a.ldxs);
+    wsbase = a.ws + (int64_t)t.group * a.ldgs;
 #pragma unroll
     for (int f = 0; f < FC; ++f)
-      wsp[f] = a.ws + (int64_t)t.group * a.ldgs + (int64_t)(t.c0 + min(wc + f * 32 + fragment_col(lane & 31), t.cn - 1)) * a.ldws;
+      wso[f] = (uint32_t)((t.c0 + min(wc + f * 32 + fragment_col(sub), t.cn - 1)) * a.ldws);
   };
   // The scales of steps b ... b + 3 in the low bytes after a shift by scale_shift(b): a word that ends with the row's last scale.
-  auto scale_word = [&](const uint8_t* p, int b) -> uint32_t {
+  const int last_word = max(steps - 4, 0);
+  auto scale_word = [&](const uint8_t* base, uint32_t offset, int b) -> uint32_t {
+    const uint8_t* p = base + min(b, last_word);  // the same for all lanes
     uint32_t w;
     if (steps >= 4) {
-      __builtin_memcpy(&w, p + min(b, steps - 4), 4);
+      __builtin_memcpy(&w, p + offset, 4);
     } else {
-      w = p[0] | (uint32_t)p[1] << 8;
-      if (steps > 2) w |= (uint32_t)p[2] << 16;
+      w = p[offset] | (uint32_t)p[offset + 1] << 8;
+      if (steps > 2) w |= (uint32_t)p[offset + 2] << 16;
     }
     return w;
   };
@@ -566,18 +612,22 @@ __global__ __launch_bounds__(512) void e4m3_tile_kernel(E4m3Args a, int col_tile
 #pragma unroll
         for (int i = 0; i < 16; ++i) acc[f][c][i] = 0.0f;
   };
-  auto fragment = [&](int buffer, int r, int kk, i32x8& f) {
-    const uint8_t* row = lds + buffer * BUFFER + r * kScaleBlock;
-    const int shift = piece_shift(r);
-    const i32x4 p = *reinterpret_cast<const i32x4*>(row + (((kk * 4 + half) ^ shift) << 4));
-    const i32x4 q = *reinterpret_cast<const i32x4*>(row + (((kk * 4 + 2 + half) ^ shift) << 4));
-    f = __builtin_shufflevector(p, q, 0, 1, 2, 3, 4, 5, 6, 7);
+  // Offsets into a buffer, of which everything that is the same for the wave is left out: it goes into the instruction.
+  const int rlane = sub * kScaleBlock + ((half ^ row_shift(sub)) << 4);
+  const int clane = fragment_col(sub) * kScaleBlock + ((half ^ col_shift(fragment_col(sub))) << 4);
+  auto fragment = [&](int first, int at, int kk, i32x8& f) {
+    const uint8_t* p = lds + first;
+    const i32x4 u = *reinterpret_cast<const i32x4*>(p + (at ^ (kk << 6)));
+    const i32x4 v = *reinterpret_cast<const i32x4*>(p + (at ^ (kk << 6 | 32)));
+    f = __builtin_shufflevector(u, v, 0, 1, 2, 3, 4, 5, 6, 7);
   };
   auto col_fragments = [&](int buffer, int kk, i32x8 (&f)[FC]) {
 #pragma unroll
-    for (int c = 0; c < FC; ++c) fragment(buffer, wc + c * 32 + fragment_col(sub), kk, f[c]);
+    for (int c = 0; c < FC; ++c) fragment(buffer * BUFFER + wc * kScaleBlock + c * 32 * kScaleBlock, clane, kk, f[c]);
   };
-  auto row_fragment = [&](int buffer, int kk, int r, i32x8& f) { fragment(buffer, wr + r * 32 + sub, kk, f); };
+  auto row_fragment = [&](int buffer, int kk, int r, i32x8& f) {
+    fragment(buffer * BUFFER + wr * kScaleBlock + r * 32 * kScaleBlock, rlane, kk, f);
+  };
   auto store = [&](const Tile& t) {
     T* base = static_cast<T*>(a.y) + t.pbegin * a.ldy + t.c0;
     const int64_t known = a.xrows * a.slots;
@@ -633,9 +683,9 @@ __global__ __launch_bounds__(512) void e4m3_tile_kernel(E4m3Args a, int col_tile
     };
     auto scales = [&](int b) {
 #pragma unroll
-      for (int f = 0; f < FR; ++f) xn[f] = scale_word(xsp[f], b);
+      for (int f = 0; f < FR; ++f) xn[f] = scale_word(a.xs, xso[f], b);
 #pragma unroll
-      for (int f = 0; f < FC; ++f) wn[f] = scale_word(wsp[f], b);
+      for (int f = 0; f < FC; ++f) wn[f] = scale_word(wsbase, wso[f], b);
     };
     auto take_scales = [&](int b) {
       const int shift = scale_shift(b);
@@ -668,7 +718,6 @@ __global__ __launch_bounds__(512) void e4m3_tile_kernel(E4m3Args a, int col_tile
     col_fragments(cnow, 0, fc[0]);
     row_fragment(rnow, 0, 0, fr[0]);
     for (;;) {
-      asm volatile("" : "+v"(sub), "+v"(half));  // LDS addresses are made anew in every step: there are no registers to keep them
       if ((done & 3) == 0 && done + 4 < steps) scales(done + 4);
 #pragma unroll
       for (int p = 0; p < FR; ++p) {
@@ -799,7 +848,8 @@ hipError_t product_typed(const E4m3Args& a, hipStream_t st) {
   const int64_t blocks = tile_bound(a.rows, a.groups, kTile, cols);
   if (blocks > 0x7fffffff) return hipErrorInvalidConfiguration;
   // 256 x 256 tiles: results of 16 bits, two steps at least, offsets of 32 bits.
-  const bool tiled = sizeof(T) == 2 && a.Kp >= 2 * kScaleBlock && a.xrows * a.ldx < (int64_t)1 << 32 && a.N * a.ldw < (int64_t)1 << 32;
+  const bool tiled = sizeof(T) == 2 && a.Kp >= 2 * kScaleBlock && a.xrows * a.ldx < (int64_t)1 << 32 && a.N * a.ldw < (int64_t)1 << 32 &&
+                     a.xrows * a.ldxs < (int64_t)1 << 32 && a.N * a.ldws < (int64_t)1 << 32;
   // Up to 4 rows a group the matrices are what takes time, and the kernel for few rows reads them as fast as any (64 groups of
   // 1024 x 2048, 64 rows 23 us, tiles 28; 256 rows 31 and 31).  Beyond, tiles read them less often (1,024 rows 46 and 32), but where
   // there are few of them a good part of the chip has nothing to do (256 rows, 4 groups of 2048 x 2048 22 us, tiles 26; 8 rows 13
@@ -818,10 +868,15 @@ hipError_t product_typed(const E4m3Args& a, hipStream_t st) {
       return hipGetLastError();
     }
   }
-  if constexpr (sizeof(T) == 4)
-    e4m3_wide_kernel<<<(uint32_t)blocks, 256, 0, st>>>(a, cols);
-  else
+  if constexpr (sizeof(T) == 4) {
+    const int wcols = (a.N + 127) / 128;
+    if (a.rows / 128 * wcols >= 512)
+      e4m3_wide_kernel<128><<<(uint32_t)tile_bound(a.rows, a.groups, 128, wcols), 256, 0, st>>>(a, wcols);
+    else
+      e4m3_wide_kernel<64><<<(uint32_t)blocks, 256, 0, st>>>(a, cols);
+  } else {
     e4m3_any_kernel<T><<<(uint32_t)blocks, 256, 0, st>>>(a, cols);
+  }
   return hipGetLastError();
 }
 

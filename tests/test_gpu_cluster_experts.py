@@ -1,0 +1,51 @@
+"""The operators of cluster experts together: k-means, assignment, training and serving of a model per cluster."""
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+
+@pytest.fixture(scope="module")
+def ce():
+    if not torch.cuda.is_available():
+        pytest.skip("needs a GPU")
+    from paper_1802_04450_amd import cluster_experts
+    return cluster_experts
+
+
+def test_example_learns_and_serves(ce):
+    errors, size, out16, out8, y = ce.example()
+    assert errors[0] == pytest.approx(size, rel=1e-5)                      # matrices of zeros
+    # within a cluster the inputs have unit covariance: the error goes down by (1 - 0.4 * 1)^2 or more a step but for the points
+    # whose second cluster has a say, until bf16's rounding (2^-8 of each of about 17 terms, squared) is what is left
+    assert errors[-1] < 1e-3 * size
+    # 8 bits: two factors, each rounded to 3 bits of fraction, 2^-4 / sqrt(3) in the mean at most
+    gap = float((out16.float() - out8.float()).norm() / out16.float().norm())
+    assert gap < 2.0 ** -4
+
+
+def test_gradients_of_the_model_against_differences(ce):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(3)
+    normal = lambda *s: torch.randn(*s, generator=g, device="cuda")
+    model = ce.ClusterExperts(2.0 * normal(5, 6), 7, t=2, width=2.0, dtype=torch.float32)
+    model.weights = normal(*model.weights.shape)
+    x, target = normal(40, 6), normal(40, 7)
+    fixed = model._rows(x, model._assign(x)[1])          # the centre that is subtracted counts as given
+    model._rows = lambda *_: fixed
+    out, saved = model.forward(x)
+    dweights, dcentres = model.backward(target, saved)
+    loss = lambda: float((model.forward(x)[0].double() * target.double()).sum())
+    for value, grad in ((model.weights, dweights), (model.centres, dcentres)):
+        v, h = normal(*grad.shape), 1e-3
+        value += h * v
+        up, same = loss(), torch.equal(model._assign(x)[1], saved.idx)
+        value -= 2 * h * v
+        down, same = loss(), same and torch.equal(model._assign(x)[1], saved.idx)
+        value += h * v
+        assert same                                                        # no row chose otherwise on the way
+        ana = float((grad.double() * v.double()).sum())
+        size = float((grad.double() * v.double()).abs().sum())
+        # fp32 rounding of 280 outputs of size 4 (about 1e-5 in all) over 2 h, and the second order
+        assert abs((up - down) / (2 * h) - ana) <= 2e-2 + 2e-3 * size

@@ -414,6 +414,20 @@ def test_grouped_product_e4m3_extreme_scales(B, kind):
     _close(y[keep], ref, size, 256, kind, more=0.0 if kind == "f32" else 2.0 ** -10)
 
 
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("rows", [1, 40, 2000])
+def test_grouped_product_e4m3_smallest_scale(B, kind, rows):
+    """Blocks whose power of two is the smallest there is, against large ones: the results are of ordinary size."""
+    rng = np.random.default_rng(rows)
+    x, w = _rounded(rng.standard_normal((rows, 200)) * 2.0 ** -126, "f32"), _rounded(rng.standard_normal((1, 24, 200)) * 2.0 ** 118, "f32")
+    xq, xs = B.sc_quantize_blocks(_dev(x, "f32"))
+    wq, ws = B.sc_quantize_blocks(_dev(w, "f32"))
+    assert int(xs.min()) == 0
+    y = B.sc_grouped_product_e4m3(xq, xs, wq, ws, torch.tensor([0, rows], dtype=torch.int32, device=DEV), dtype=TYPES[kind])
+    xv, wv = ox.quantize_blocks(x)[2], ox.quantize_blocks(w[0])[2]
+    _close(y, *ox.grouped_product(xv, wv[None], [0, rows]), 256, kind, more=0.0 if kind == "f32" else 2.0 ** -10)
+
+
 # ---- how the calls behave ---------------------------------------------------------------------------------------------
 def _step(B, scores, x, w, dout):
     idx, weight, offsets, order, place = B.sc_route(scores, 2)
