@@ -532,32 +532,36 @@ def _enqueue(device, call, *args) -> None:
     and the stream object cost (5 us) is left out where the device is the current one."""
     import torch
     if torch.cuda.current_device() == device.index:
-        _check(call(*args, torch._C._cuda_getCurrentRawStream(device.index)))
+        code = call(*args, torch._C._cuda_getCurrentRawStream(device.index))
     else:
         with torch.cuda.device(device):
-            _check(call(*args, torch._C._cuda_getCurrentRawStream(device.index)))
+            code = call(*args, torch._C._cuda_getCurrentRawStream(device.index))
+    if code:
+        _check(code)
 
 
 def _matrix(t, device=None):
     """A device tensor of one of the three types whose rows are contiguous (strided rows are taken as they are)."""
     _dtype(t.dtype)
     assert t.is_cuda and (device is None or t.device == device), (t.device, device)
-    assert t.numel() == 0 or t.shape[-1] <= 1 or t.stride(-1) == 1, t.stride()
+    assert t.stride(-1) == 1 or t.shape[-1] <= 1 or t.numel() == 0, t.stride()
     return t
 
 
 def _ld(t, dim: int = 0) -> int:
     """Row stride of a matrix in elements (that of a single row does not matter)."""
+    if t.shape[dim] > 1:
+        return t.stride(dim)
     least = t.shape[-1]
     for d in range(dim + 1, t.dim() - 1):
         least *= t.shape[d]
-    return t.stride(dim) if t.shape[dim] > 1 else max(least, 1)
+    return max(least, 1)
 
 
 def _ints(t, count, device):
     import torch
-    _dev(t, torch.int32)
-    assert t.device == device and (count is None or t.numel() == count), (t.device, t.shape, count)
+    assert t.dtype == torch.int32 and t.device == device and t.is_contiguous(), (t.dtype, t.device, t.is_contiguous())
+    assert count is None or t.numel() == count, (t.shape, count)
     return t
 
 
@@ -584,7 +588,7 @@ def sc_route(scores, t: int, allowed=None, normalize: bool = True):
     weight = torch.empty((n, slots), dtype=torch.float32, device=dev)
     offsets = torch.empty(k + 1, dtype=torch.int32, device=dev)
     order = torch.empty(n * slots, dtype=torch.int32, device=dev)
-    place = torch.empty((n, slots), dtype=torch.int32, device=dev)
+    place = torch.empty_like(idx)
     need = ctypes.c_size_t(0)
     _check(lib().sc_route_workspace_bytes(n, k, t, ctypes.byref(need)))
     work = torch.empty(need.value, dtype=torch.uint8, device=dev)

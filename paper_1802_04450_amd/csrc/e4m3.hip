@@ -368,9 +368,8 @@ __global__ __launch_bounds__(256, 2) void e4m3_wide_kernel(E4m3Args a, int cols)
 #pragma unroll
     for (int v = 0; v < F; ++v) {
       const int col = wc + v * 16 + quad * 4;
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (col + i < cn) out[col + i] = acc[u][v][i];
+      const float q[4] = {acc[u][v][0], acc[u][v][1], acc[u][v][2], acc[u][v][3]};
+      store_any(out + col, q, cn - col);
     }
   }
 }
@@ -382,7 +381,7 @@ __global__ __launch_bounds__(256, 2) void e4m3_wide_kernel(E4m3Args a, int cols)
 constexpr int kThinRun = 2;
 
 template <typename T, int RF, int KS>
-__global__ __launch_bounds__(KS > 4 ? KS * 64 : 256) void e4m3_thin_kernel(E4m3Args a, int col_tiles, int whole_stores) {
+__global__ __launch_bounds__(KS > 4 ? KS * 64 : 256) void e4m3_thin_kernel(E4m3Args a, int col_tiles) {
   constexpr int CT = KS > 4 ? 1 : 4 / KS;
   constexpr bool WIDE = sizeof(T) == 4;
   __shared__ f32x4 part[KS > 1 ? (KS - 1) * CT * RF * 64 : 1];
@@ -486,22 +485,15 @@ __global__ __launch_bounds__(KS > 4 ? KS * 64 : 256) void e4m3_thin_kernel(E4m3A
 #pragma unroll
       for (int r = 0; r < RF; ++r) acc[r] += part[((q * CT + ct) * RF + r) * 64 + lane];
   }
-  typedef T Quad __attribute__((ext_vector_type(4)));
 #pragma unroll
   for (int r = 0; r < RF; ++r) {
     const int row = r * 16 + sub, col = c0 + quad * 4;
     if (row >= t.count || col >= a.N) continue;
     T* out = static_cast<T*>(a.y) + (t.begin + row) * a.ldy + col;
-    Quad q;
+    T q[4];
 #pragma unroll
     for (int u = 0; u < 4; ++u) q[u] = static_cast<T>(acc[r][u]);
-    if (whole_stores) {
-      *reinterpret_cast<Quad*>(out) = q;
-    } else {
-#pragma unroll
-      for (int u = 0; u < 4; ++u)
-        if (col + u < a.N) out[u] = q[u];
-    }
+    store_any(out, q, a.N - col);
   }
 }
 
@@ -522,7 +514,7 @@ __device__ __forceinline__ int col_shift(int c) { return (c & 2) | ((c >> 1) & 4
 __device__ __forceinline__ int fragment_col(int i) { return (i & 0x13) | ((i & 4) << 1) | ((i & 8) >> 1); }
 
 template <typename T>
-__global__ __launch_bounds__(512) void e4m3_tile_kernel(E4m3Args a, int col_tiles, int whole_stores) {
+__global__ __launch_bounds__(512) void e4m3_tile_kernel(E4m3Args a, int col_tiles) {
   constexpr int BM = 256, BN = 256, WC = 4, NW = 8, FR = 4, FC = 2, LOADS = 4;
   constexpr int BUFFER = BM * kScaleBlock;
   __shared__ __attribute__((aligned(1024))) uint8_t lds[5 * BUFFER];
@@ -631,7 +623,6 @@ __global__ __launch_bounds__(512) void e4m3_tile_kernel(E4m3Args a, int col_tile
   auto store = [&](const Tile& t) {
     T* base = static_cast<T*>(a.y) + t.pbegin * a.ldy + t.c0;
     const int64_t known = a.xrows * a.slots;
-    typedef T Part __attribute__((ext_vector_type(8)));
 #pragma unroll
     for (int f = 0; f < FR; ++f) {
       const int row = wr + f * 32 + (lane & 31);
@@ -643,16 +634,10 @@ __global__ __launch_bounds__(512) void e4m3_tile_kernel(E4m3Args a, int col_tile
         for (int g = 0; g < 2; ++g) {
           const int col = wc + c * 32 + g * 16 + (lane >> 5) * 8;
           T* out = base + row * a.ldy + col;
-          Part q;
+          T q[8];
 #pragma unroll
           for (int u = 0; u < 8; ++u) q[u] = static_cast<T>(none ? 0.0f : acc[f][c][g * 8 + u]);
-          if (whole_stores) {
-            if (col < t.cn) *reinterpret_cast<Part*>(out) = q;
-          } else {
-#pragma unroll
-            for (int u = 0; u < 8; ++u)
-              if (col + u < t.cn) out[u] = q[u];
-          }
+          store_any(out, q, t.cn - col);
         }
     }
   };
@@ -730,9 +715,7 @@ __global__ __launch_bounds__(512) void e4m3_tile_kernel(E4m3Args a, int col_tile
         }
         fetch_col(p, ahead, at);
         __builtin_amdgcn_sched_barrier(0);
-        __builtin_amdgcn_s_setprio(1);
         multiply(p, fr[p & 1], fc[0]);
-        __builtin_amdgcn_s_setprio(0);
       }
 #pragma unroll
       for (int p = 0; p < FR; ++p) {
@@ -751,9 +734,7 @@ __global__ __launch_bounds__(512) void e4m3_tile_kernel(E4m3Args a, int col_tile
           fetch_row(3, cnow, at);
         }
         __builtin_amdgcn_sched_barrier(0);
-        __builtin_amdgcn_s_setprio(1);
         multiply(p, fr[p & 1], fc[1]);
-        __builtin_amdgcn_s_setprio(0);
       }
       const int free = rnow, filled = cnow;
       cnow = cnext;
@@ -828,17 +809,16 @@ hipError_t thin_typed(const E4m3Args& a, hipStream_t st) {
   const int cols = (tiles + per_group - 1) / per_group;
   const int64_t blocks = tile_bound(a.rows, a.groups, RF * 16, cols);
   if (blocks > 0x7fffffff) return hipErrorInvalidConfiguration;
-  const int whole = a.N % 4 == 0 && a.ldy % 4 == 0 && reinterpret_cast<uintptr_t>(a.y) % (4 * sizeof(T)) == 0;
   if (ks == 1)
-    e4m3_thin_kernel<T, RF, 1><<<(uint32_t)blocks, 256, 0, st>>>(a, cols, whole);
+    e4m3_thin_kernel<T, RF, 1><<<(uint32_t)blocks, 256, 0, st>>>(a, cols);
   else if (ks == 2)
-    e4m3_thin_kernel<T, RF, 2><<<(uint32_t)blocks, 256, 0, st>>>(a, cols, whole);
+    e4m3_thin_kernel<T, RF, 2><<<(uint32_t)blocks, 256, 0, st>>>(a, cols);
   else if (ks == 4)
-    e4m3_thin_kernel<T, RF, 4><<<(uint32_t)blocks, 256, 0, st>>>(a, cols, whole);
+    e4m3_thin_kernel<T, RF, 4><<<(uint32_t)blocks, 256, 0, st>>>(a, cols);
   else if (ks == 8)
-    e4m3_thin_kernel<T, RF, 8><<<(uint32_t)blocks, 512, 0, st>>>(a, cols, whole);
+    e4m3_thin_kernel<T, RF, 8><<<(uint32_t)blocks, 512, 0, st>>>(a, cols);
   else if constexpr (RF <= 2)  // registers of 16 waves
-    e4m3_thin_kernel<T, RF, 16><<<(uint32_t)blocks, 1024, 0, st>>>(a, cols, whole);
+    e4m3_thin_kernel<T, RF, 16><<<(uint32_t)blocks, 1024, 0, st>>>(a, cols);
   return hipGetLastError();
 }
 
@@ -863,8 +843,7 @@ hipError_t product_typed(const E4m3Args& a, hipStream_t st) {
     if (tiled) {
       const int wcols = (a.N + 255) / 256;
       const int64_t n = tile_bound(a.rows, a.groups, 256, wcols);
-      const int whole = a.N % 8 == 0 && a.ldy % 8 == 0 && reinterpret_cast<uintptr_t>(a.y) % 16 == 0;
-      e4m3_tile_kernel<T><<<(uint32_t)(n < 256 ? n : 256), 512, 0, st>>>(a, wcols, whole);
+      e4m3_tile_kernel<T><<<(uint32_t)(n < 256 ? n : 256), 512, 0, st>>>(a, wcols);
       return hipGetLastError();
     }
   }

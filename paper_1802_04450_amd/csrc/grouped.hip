@@ -76,7 +76,7 @@ __global__ __launch_bounds__(256) void grouped_any_kernel(const T* __restrict__ 
                                                           const int32_t* __restrict__ offsets, const int32_t* __restrict__ order,
                                                           int64_t ldr, int64_t ldc, int64_t ldg, int64_t ldo, int64_t ldog,
                                                           int64_t rows, int64_t xrows, int groups, int slots, int outr, int outc,
-                                                          int depth, int row_tiles, int col_tiles, Parts parts, int whole_stores) {
+                                                          int depth, int row_tiles, int col_tiles, Parts parts) {
   typedef typename Matrix<T>::Chunk Chunk;
   constexpr int CH = Matrix<T>::kChunk;
   constexpr int BK = 4 * CH * U;
@@ -246,22 +246,14 @@ __global__ __launch_bounds__(256) void grouped_any_kernel(const T* __restrict__ 
       const int col = wc + b * 16 + quad * 4;
       if (col >= cn) continue;
       if (FORM == kGradient && sums) {
-#pragma unroll
-        for (int u = 0; u < 4; ++u)
-          if (col + u < cn) sums[(int64_t)row * outc + col + u] = acc[a][b][u];
+        const float sum[4] = {acc[a][b][0], acc[a][b][1], acc[a][b][2], acc[a][b][3]};
+        store_any(sums + (int64_t)row * outc + col, sum, cn - col);
         continue;
       }
-      typedef T Quad __attribute__((ext_vector_type(4)));
-      Quad q;
+      T q[4];
 #pragma unroll
       for (int u = 0; u < 4; ++u) q[u] = static_cast<T>(acc[a][b][u]);
-      if (whole_stores) {
-        *reinterpret_cast<Quad*>(orow + col) = q;
-      } else {
-#pragma unroll
-        for (int u = 0; u < 4; ++u)
-          if (col + u < cn) orow[col + u] = q[u];
-      }
+      store_any(orow + col, q, cn - col);
     }
   }
 }
@@ -291,7 +283,7 @@ __global__ __launch_bounds__(256) void gradient_sum_kernel(Parts parts, const in
 constexpr int kThinRun = 4;
 
 template <typename T, int RF, int KS>
-__global__ __launch_bounds__(KS > 4 ? KS * 64 : 256) void grouped_thin_kernel(GroupedArgs a, int col_tiles, int whole_stores) {
+__global__ __launch_bounds__(KS > 4 ? KS * 64 : 256) void grouped_thin_kernel(GroupedArgs a, int col_tiles) {
   typedef typename Matrix<T>::Chunk Chunk;
   constexpr int CH = Matrix<T>::kChunk, CT = KS > 4 ? 1 : 4 / KS, BK = 4 * CH;
   __shared__ f32x4 part[KS > 1 ? (KS - 1) * CT * RF * 64 : 1];
@@ -353,22 +345,15 @@ __global__ __launch_bounds__(KS > 4 ? KS * 64 : 256) void grouped_thin_kernel(Gr
 #pragma unroll
       for (int r = 0; r < RF; ++r) acc[r] += part[((q * CT + ct) * RF + r) * 64 + lane];
   }
-  typedef T Quad __attribute__((ext_vector_type(4)));
 #pragma unroll
   for (int r = 0; r < RF; ++r) {
     const int row = r * 16 + sub, col = c0 + quad * 4;
     if (row >= t.count || col >= a.N) continue;
     T* out = static_cast<T*>(a.y) + (t.begin + row) * a.ldy + col;
-    Quad q;
+    T q[4];
 #pragma unroll
     for (int u = 0; u < 4; ++u) q[u] = static_cast<T>(acc[r][u]);
-    if (whole_stores) {
-      *reinterpret_cast<Quad*>(out) = q;
-    } else {
-#pragma unroll
-      for (int u = 0; u < 4; ++u)
-        if (col + u < a.N) out[u] = q[u];
-    }
+    store_any(out, q, a.N - col);
   }
 }
 
@@ -746,9 +731,7 @@ __global__ __launch_bounds__(WR * WC * 64) void grouped_tile_kernel(TileArgs a) 
 #pragma unroll
         for (int u = 0; u < CL; ++u) fetch_col(p * CL + u, ahead);
         __builtin_amdgcn_sched_barrier(0);
-        __builtin_amdgcn_s_setprio(1);
         multiply(p, fr[p & 1], fc[0]);
-        __builtin_amdgcn_s_setprio(0);
       }
 #pragma unroll
       for (int p = 0; p < PAIRS; ++p) {
@@ -770,9 +753,7 @@ __global__ __launch_bounds__(WR * WC * 64) void grouped_tile_kernel(TileArgs a) 
           for (int u = EARLY; u < LR; ++u) fetch_row(u, cnow);
         }
         __builtin_amdgcn_sched_barrier(0);
-        __builtin_amdgcn_s_setprio(1);
         multiply(p, fr[p & 1], fc[1]);
-        __builtin_amdgcn_s_setprio(0);
       }
       const int free = rnow, filled = cnow;
       cnow = cnext;
@@ -823,17 +804,16 @@ hipError_t thin_typed(const GroupedArgs& a, hipStream_t st) {
   const int cols = (tiles + per_group - 1) / per_group;
   const int64_t blocks = tile_bound(a.rows, a.groups, RF * 16, cols);
   if (blocks > 0x7fffffff) return hipErrorInvalidConfiguration;
-  const int whole = a.N % 4 == 0 && a.ldy % 4 == 0 && reinterpret_cast<uintptr_t>(a.y) % (4 * sizeof(T)) == 0;
   if (ks == 1)
-    grouped_thin_kernel<T, RF, 1><<<(uint32_t)blocks, 256, 0, st>>>(a, cols, whole);
+    grouped_thin_kernel<T, RF, 1><<<(uint32_t)blocks, 256, 0, st>>>(a, cols);
   else if (ks == 2)
-    grouped_thin_kernel<T, RF, 2><<<(uint32_t)blocks, 256, 0, st>>>(a, cols, whole);
+    grouped_thin_kernel<T, RF, 2><<<(uint32_t)blocks, 256, 0, st>>>(a, cols);
   else if (ks == 4)
-    grouped_thin_kernel<T, RF, 4><<<(uint32_t)blocks, 256, 0, st>>>(a, cols, whole);
+    grouped_thin_kernel<T, RF, 4><<<(uint32_t)blocks, 256, 0, st>>>(a, cols);
   else if (ks == 8)
-    grouped_thin_kernel<T, RF, 8><<<(uint32_t)blocks, 512, 0, st>>>(a, cols, whole);
+    grouped_thin_kernel<T, RF, 8><<<(uint32_t)blocks, 512, 0, st>>>(a, cols);
   else if constexpr (RF <= 2)  // registers of 16 waves
-    grouped_thin_kernel<T, RF, 16><<<(uint32_t)blocks, 1024, 0, st>>>(a, cols, whole);
+    grouped_thin_kernel<T, RF, 16><<<(uint32_t)blocks, 1024, 0, st>>>(a, cols);
   return hipGetLastError();
 }
 
@@ -848,10 +828,9 @@ hipError_t any_typed(const GroupedArgs& a, int outc, int depth, hipStream_t st) 
   const int cols = (outc + TILE - 1) / TILE;
   const int64_t blocks = tile_bound(a.rows, a.groups, TILE, cols);
   if (blocks > 0x7fffffff) return hipErrorInvalidConfiguration;
-  const int whole = outc % 4 == 0 && a.ldy % 4 == 0 && reinterpret_cast<uintptr_t>(a.y) % (4 * sizeof(T)) == 0;
   grouped_any_kernel<T, FORM, TILE, TILE == 64 ? 2 : 1><<<(uint32_t)blocks, 256, 0, st>>>(
       static_cast<const T*>(a.x), static_cast<const T*>(a.w), static_cast<T*>(a.y), a.offsets, a.order, a.ldx, a.ldw, a.ldg, a.ldy, 0,
-      a.rows, a.xrows, a.groups, a.slots, 0, outc, depth, 0, cols, Parts{0, nullptr}, whole);
+      a.rows, a.xrows, a.groups, a.slots, 0, outc, depth, 0, cols, Parts{0, nullptr});
   return hipGetLastError();
 }
 
@@ -913,7 +892,7 @@ GradientCut gradient_cut(int64_t rows, int groups, int N, int K, int dtype) {
     c.side = 128, c.tiles = large;
   else
     c.side = 64, c.tiles = small;
-  const int64_t want = c.side == 256 ? 256 : c.side == 128 ? 1024 : 2048;  // workgroups
+  const int64_t want = c.side == 256 ? 256 : c.side == 128 ? 512 : 1024;  // workgroups
   c.part = 0;
   c.parts = 0;
   if (groups * c.tiles * 2 <= want && rows > 256) {
@@ -932,10 +911,9 @@ hipError_t any_gradient(const GradientArgs& a, const GradientCut& c, const Parts
   const int rt = (a.N + TILE - 1) / TILE, ct = (a.K + TILE - 1) / TILE;
   const int64_t blocks = (c.part ? c.parts : a.groups) * rt * ct;
   if (blocks > 0x7fffffff) return hipErrorInvalidConfiguration;
-  const int whole = a.K % 4 == 0 && a.ldw % 4 == 0 && a.ldg % 4 == 0 && reinterpret_cast<uintptr_t>(a.dw) % (4 * sizeof(T)) == 0;
   grouped_any_kernel<T, kGradient, TILE, TILE == 64 ? 2 : 1><<<(uint32_t)blocks, 256, 0, st>>>(
       static_cast<const T*>(a.dy), static_cast<const T*>(a.x), static_cast<T*>(a.dw), a.offsets, a.order, a.lddy, a.ldx, 0, a.ldw,
-      a.ldg, a.rows, a.xrows, a.groups, a.slots, a.N, a.K, 0, rt, ct, parts, whole);
+      a.ldg, a.rows, a.xrows, a.groups, a.slots, a.N, a.K, 0, rt, ct, parts);
   return hipGetLastError();
 }
 

@@ -241,6 +241,18 @@ __device__ __forceinline__ void meet() {
 // All LDS reads of all waves so far are done.
 __device__ __forceinline__ void read_by_all() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
+// Neighbouring results, of which `left` exist, to a place that may begin anywhere.
+template <typename T, int N>
+__device__ __forceinline__ void store_any(T* p, const T (&v)[N], int left) {
+  if (left >= N) {
+    __builtin_memcpy(p, v, sizeof(v));
+  } else {
+#pragma unroll
+    for (int u = 0; u < N; ++u)
+      if (u < left) p[u] = v[u];
+  }
+}
+
 // Source row of row p of a group, or -1: what `order` holds beyond [0, xrows * slots) reads as a row of zeros.
 __device__ __forceinline__ int64_t source_row(const int32_t* order, int64_t p, int slots, int64_t xrows) {
   const int64_t r = order ? (order[p] < 0 ? -1 : (int64_t)((uint32_t)order[p] / (uint32_t)slots)) : p;
