@@ -513,11 +513,12 @@ __device__ __forceinline__ int col_shift(int c) { return (c & 2) | ((c >> 1) & 4
 // four are eight neighbours.
 __device__ __forceinline__ int fragment_col(int i) { return (i & 0x13) | ((i & 4) << 1) | ((i & 8) >> 1); }
 
-template <typename T>
-__global__ __launch_bounds__(512) void e4m3_tile_kernel(E4m3Args a, int col_tiles) {
-  constexpr int BM = 256, BN = 256, WC = 4, NW = 8, FR = 4, FC = 2, LOADS = 4;
-  constexpr int BUFFER = BM * kScaleBlock;
-  __shared__ __attribute__((aligned(1024))) uint8_t lds[5 * BUFFER];
+#ifdef __HIP_DEVICE_COMPILE__
+// All tiles of BM rows of a workgroup, or (HALF) its one piece of half a tile.
+template <typename T, int BM, bool HALF>
+__device__ __forceinline__ void run_tiles(const E4m3Args& a, uint8_t* lds, const TileWalk<256>& walk) {
+  constexpr int BN = 256, WC = 4, NW = 8, FR = BM / 64, FC = 2, RLOADS = BM / 64, CLOADS = 4;
+  constexpr int BUFFER = 256 * kScaleBlock;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wr = wave / WC * (FR * 32), wc = wave % WC * (FC * 32);
@@ -525,9 +526,8 @@ __global__ __launch_bounds__(512) void e4m3_tile_kernel(E4m3Args a, int col_tile
     int group, rn, c0, cn;
     int64_t pbegin;
   };
-  const TileWalk<BM> walk(a.offsets, a.groups, a.rows, col_tiles);
   auto tile_at = [&](int64_t i) {
-    const RowTile r = walk.at(i);
+    const RowTile r = HALF ? walk.half() : walk.at(i);
     Tile t;
     t.group = r.group;
     t.rn = r.count;
@@ -542,26 +542,28 @@ __global__ __launch_bounds__(512) void e4m3_tile_kernel(E4m3Args a, int col_tile
   const __amdgpu_buffer_rsrc_t xres =
       __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(a.x), 0, (int)(uint32_t)(a.xrows * a.ldx), 0x00027000);
   __amdgpu_buffer_rsrc_t wres = xres;
-  uint32_t ro[LOADS], co[LOADS];
+  uint32_t ro[RLOADS], co[CLOADS];
   const int eight = lane >> 3;
-  int32_t look[LOADS], looks[FR];  // source rows of the next tile: that the lane loads, whose scales it needs
+  int32_t look[RLOADS], looks[FR];  // source rows of the next tile: that the lane loads, whose scales it needs
   uint32_t xso[FR], wso[FC];  // where the scales of the lane's rows and columns begin
   const uint8_t* wsbase = a.ws;
   const int sub = lane & 31, half = lane >> 5;
   auto look_up = [&](const Tile& t) {
 #pragma unroll
-    for (int u = 0; u < LOADS; ++u)
-      look[u] = (int32_t)source_row(a.order, t.pbegin + min((wave * LOADS + u) * 8 + eight, t.rn - 1), a.slots, a.xrows);
+    for (int u = 0; u < RLOADS; ++u)
+      look[u] = (int32_t)source_row(a.order, t.pbegin + min((wave * RLOADS + u) * 8 + eight, t.rn - 1), a.slots, a.xrows);
 #pragma unroll
     for (int f = 0; f < FR; ++f)
       looks[f] = (int32_t)source_row(a.order, t.pbegin + min(wr + f * 32 + (lane & 31), t.rn - 1), a.slots, a.xrows);
   };
   auto begin = [&](const Tile& t) {
 #pragma unroll
-    for (int u = 0; u < LOADS; ++u) {
-      const int r = (wave * LOADS + u) * 8 + eight;
-      ro[u] = (uint32_t)(max(look[u], 0) * a.ldx + ((lane & 7) ^ row_shift(r)) * 16);
-      co[u] = (uint32_t)((int64_t)(t.c0 + min(r, t.cn - 1)) * a.ldw + ((lane & 7) ^ col_shift(r)) * 16);
+    for (int u = 0; u < RLOADS; ++u)
+      ro[u] = (uint32_t)(max(look[u], 0) * a.ldx + ((lane & 7) ^ row_shift((wave * RLOADS + u) * 8 + eight)) * 16);
+#pragma unroll
+    for (int u = 0; u < CLOADS; ++u) {
+      const int c = (wave * CLOADS + u) * 8 + eight;
+      co[u] = (uint32_t)((int64_t)(t.c0 + min(c, t.cn - 1)) * a.ldw + ((lane & 7) ^ col_shift(c)) * 16);
     }
     wres = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(a.w) + (int64_t)t.group * a.ldg, 0,
                                              (int)(uint32_t)((int64_t)(a.N - 1) * a.ldw + a.Kp), 0x00027000);
@@ -589,10 +591,10 @@ __global__ __launch_bounds__(512) void e4m3_tile_kernel(E4m3Args a, int col_tile
   };
   auto scale_shift = [&](int b) { return steps >= 4 ? 8 * (b - min(b, steps - 4)) : 0; };
   auto fetch_row = [&](int u, int buffer, int at) {
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(xres, (LdsVoid*)(lds + buffer * BUFFER + (wave * LOADS + u) * 1024), 16, ro[u], at, 0, 0);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(xres, (LdsVoid*)(lds + buffer * BUFFER + (wave * RLOADS + u) * 1024), 16, ro[u], at, 0, 0);
   };
   auto fetch_col = [&](int u, int buffer, int at) {
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(wres, (LdsVoid*)(lds + buffer * BUFFER + (wave * LOADS + u) * 1024), 16, co[u], at, 0, 0);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(wres, (LdsVoid*)(lds + buffer * BUFFER + (wave * CLOADS + u) * 1024), 16, co[u], at, 0, 0);
   };
 
   f32x16 acc[FR][FC];
@@ -642,7 +644,8 @@ __global__ __launch_bounds__(512) void e4m3_tile_kernel(E4m3Args a, int col_tile
     }
   };
 
-  if (walk.count > 0) {
+  const int64_t count = HALF ? (walk.half().group >= 0 ? 1 : 0) : walk.count;
+  if (count > 0) {
     int64_t index = 0;
     Tile tile = tile_at(0), next = tile;
     clear();
@@ -651,7 +654,7 @@ __global__ __launch_bounds__(512) void e4m3_tile_kernel(E4m3Args a, int col_tile
     bool more;
     int done = 0, at = 0;  // steps of the tile that are done; where the loads stand, in bytes along the contraction
     auto look_ahead = [&]() {
-      more = index + 1 < walk.count;
+      more = index + 1 < count;
       if (more) {
         next = tile_at(index + 1);
         look_up(next);
@@ -684,6 +687,7 @@ __global__ __launch_bounds__(512) void e4m3_tile_kernel(E4m3Args a, int col_tile
       for (int u = 0; u < FC; ++u)
         acc[r][u] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(c[u], f, acc[r][u], 0, 0, 0, ww[u], 0, xw[r]);
     };
+    constexpr int EARLY = FR > 2 ? FR - 2 : 0;  // loads of the rows' operand before the second meeting
     int cnow = 0, rnow = 1, cnext = 2, rnext = 3, ahead = 4;  // buffers of this step, of the next one, and the free one
     look_up(tile);
     begin(tile);
@@ -694,12 +698,12 @@ __global__ __launch_bounds__(512) void e4m3_tile_kernel(E4m3Args a, int col_tile
 #pragma unroll
     for (int f = 0; f < 2; ++f) {
 #pragma unroll
-      for (int u = 0; u < LOADS; ++u) fetch_col(u, f ? cnext : cnow, at);
+      for (int u = 0; u < CLOADS; ++u) fetch_col(u, f ? cnext : cnow, at);
 #pragma unroll
-      for (int u = 0; u < LOADS; ++u) fetch_row(u, f ? rnext : rnow, at);
+      for (int u = 0; u < RLOADS; ++u) fetch_row(u, f ? rnext : rnow, at);
       advance();
     }
-    meet<2 * LOADS>();
+    meet<RLOADS + CLOADS>();
     col_fragments(cnow, 0, fc[0]);
     row_fragment(rnow, 0, 0, fr[0]);
     for (;;) {
@@ -713,25 +717,26 @@ __global__ __launch_bounds__(512) void e4m3_tile_kernel(E4m3Args a, int col_tile
           col_fragments(cnow, 1, fc[1]);
           row_fragment(rnow, 1, 0, fr[0]);
         }
-        fetch_col(p, ahead, at);
+#pragma unroll
+        for (int u = 0; u < CLOADS / FR; ++u) fetch_col(p * (CLOADS / FR) + u, ahead, at);
         __builtin_amdgcn_sched_barrier(0);
         multiply(p, fr[p & 1], fc[0]);
       }
 #pragma unroll
       for (int p = 0; p < FR; ++p) {
         __builtin_amdgcn_sched_barrier(0);
-        if (p == 1) read_by_all();
+        if (p == 1 && FR > 2) read_by_all();
         if (p + 1 < FR) {
           row_fragment(rnow, 1, p + 1, fr[(p + 1) & 1]);
         } else {
-          meet<LOADS + 2>();
+          meet<CLOADS + EARLY>();
           col_fragments(cnext, 0, fc[0]);
           row_fragment(rnext, 0, 0, fr[0]);
         }
-        if (p == 1 || p == 2) fetch_row(p - 1, cnow, at);
-        if (p == 3) {
-          fetch_row(2, cnow, at);
-          fetch_row(3, cnow, at);
+        if (p >= 1 && p + 1 < FR) fetch_row(p - 1, cnow, at);
+        if (p + 1 == FR) {
+#pragma unroll
+          for (int u = EARLY; u < RLOADS; ++u) fetch_row(u, cnow, at);
         }
         __builtin_amdgcn_sched_barrier(0);
         multiply(p, fr[p & 1], fc[1]);
@@ -764,13 +769,25 @@ __global__ __launch_bounds__(512) void e4m3_tile_kernel(E4m3Args a, int col_tile
       }
       advance();
     }
-    arrived();  // nothing may still be on its way into LDS when the workgroup gives it back
+    arrived();  // nothing may still be on its way into LDS when the workgroup gives it back, or fills it anew
   }
+}
+#endif
+
+template <typename T>
+__global__ __launch_bounds__(512) void e4m3_tile_kernel(E4m3Args a, int col_tiles) {
+#ifdef __HIP_DEVICE_COMPILE__  // the buffer loads' types exist for the device only: for the host a kernel is its name
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[5 * 256 * kScaleBlock];
+  const TileWalk<256> walk(a.offsets, a.groups, a.rows, col_tiles);
+  run_tiles<T, 256, false>(a, lds, walk);
+  __syncthreads();
+  run_tiles<T, 128, true>(a, lds, walk);
   // rows behind the last group
   const GroupRange g = group_range(a.offsets, a.groups, a.rows, a.groups);
   const int64_t count = (g.end - g.begin) * a.N;
-  for (int64_t i = (int64_t)blockIdx.x * (NW * 64) + tid; i < count; i += (int64_t)gridDim.x * (NW * 64))
+  for (int64_t i = (int64_t)blockIdx.x * 512 + threadIdx.x; i < count; i += (int64_t)gridDim.x * 512)
     static_cast<T*>(a.y)[(g.begin + i / a.N) * a.ldy + i % a.N] = static_cast<T>(0.0f);
+#endif
 }
 
 template <typename T>
@@ -842,7 +859,7 @@ hipError_t product_typed(const E4m3Args& a, hipStream_t st) {
   if constexpr (sizeof(T) == 2) {
     if (tiled) {
       const int wcols = (a.N + 255) / 256;
-      const int64_t n = tile_bound(a.rows, a.groups, 256, wcols);
+      const int64_t n = 2 * tile_bound(a.rows, a.groups, 256, wcols);  // pieces of half a tile
       e4m3_tile_kernel<T><<<(uint32_t)(n < 256 ? n : 256), 512, 0, st>>>(a, wcols);
       return hipGetLastError();
     }

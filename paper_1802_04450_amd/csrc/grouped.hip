@@ -409,8 +409,9 @@ struct TileArgs {
   Parts parts;
 };
 
-template <typename T, int FORM, int BM, int BN, int WR, int WC>
-__global__ __launch_bounds__(WR * WC * 64) void grouped_tile_kernel(TileArgs a) {
+// All tiles of BM rows of a workgroup, or (HALF) its one piece of half a tile.
+template <typename T, int FORM, int BM, int BN, int WR, int WC, bool HALF>
+__device__ __forceinline__ void run_tiles(const TileArgs& a, char* lds, const TileWalk<HALF ? 2 * BM : BM>& walk) {
   typedef typename Matrix<T>::Chunk Chunk;
   typedef T Part __attribute__((ext_vector_type(8)));
   constexpr int NW = WR * WC;
@@ -418,8 +419,7 @@ __global__ __launch_bounds__(WR * WC * 64) void grouped_tile_kernel(TileArgs a) 
   constexpr bool R_ALONG = FORM != kGradient, C_ALONG = FORM == kProduct;
   constexpr int LR = BM / 8 / NW, LC = BN / 8 / NW;  // loads of 1 KB a wave and step
   static_assert(LR * 8 * NW == BM && LC * 8 * NW == BN && FR % 4 == 0 && FC % 2 == 0, "");
-  constexpr int BUFFERS = 5, BUFFER = (BM > BN ? BM : BN) * kStep * 2;  // bytes
-  __shared__ __attribute__((aligned(1024))) char lds[BUFFERS * BUFFER];
+  constexpr int BUFFER = (BM > BN ? BM : BN) * kStep * 2;  // bytes
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wr = wave / WC * (BM / WR), wc = wave % WC * (BN / WC);
@@ -430,15 +430,14 @@ __global__ __launch_bounds__(WR * WC * 64) void grouped_tile_kernel(TileArgs a) 
     int64_t pbegin;
     int length;
   };
-  const TileWalk<BM> walk(a.offsets, FORM == kGradient ? 0 : a.groups, a.rows, FORM == kGradient ? 1 : a.col_tiles);
   const GroupOrder by_length(a.offsets, FORM == kGradient && !a.parts.part ? a.groups : 0, a.rows);
   const PartList part_list(a.offsets, FORM == kGradient && a.parts.part ? a.groups : 0, a.rows, a.parts.part);
   const int per_group = a.row_tiles * a.col_tiles;  // gradient
   const int64_t group_parts = FORM != kGradient ? 0 : a.parts.part ? part_list.total : a.groups;
   // A gradient's tiles take as long as their groups are.  From the longest group to the shortest they are dealt out to all
   // workgroups, to and fro.
-  const int64_t count = FORM == kGradient ? (group_parts * per_group + gridDim.x - 1) / gridDim.x : walk.count;
-  auto tile_at = [&](int64_t i, Tile& t) {  // false: there is none (only the last one of a gradient)
+  const int64_t count = FORM == kGradient ? (group_parts * per_group + gridDim.x - 1) / gridDim.x : HALF ? 1 : walk.count;
+  auto tile_at = [&](int64_t i, Tile& t) {  // false: there is none (the last one of a gradient, the half)
     if (FORM == kGradient) {
       const int64_t at = i * gridDim.x + (i & 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
       if (at >= group_parts * per_group) return false;
@@ -458,7 +457,8 @@ __global__ __launch_bounds__(WR * WC * 64) void grouped_tile_kernel(TileArgs a) 
         t.length = (int)(r.end - r.begin);
       }
     } else {
-      const RowTile r = walk.at(i);
+      const RowTile r = HALF ? walk.half() : walk.at(i);
+      if (HALF && r.group < 0) return false;
       t.group = r.group;
       t.r0 = 0;
       t.rn = r.count;
@@ -772,17 +772,27 @@ __global__ __launch_bounds__(WR * WC * 64) void grouped_tile_kernel(TileArgs a) 
       }
       advance();
     }
-    arrived();  // nothing may still be on its way into LDS when the workgroup gives it back
+    arrived();  // nothing may still be on its way into LDS when the workgroup gives it back, or fills it anew
   }
+}
 
-  if (FORM != kGradient) {  // rows behind the last group
+template <typename T, int FORM>
+__global__ __launch_bounds__(512) void grouped_tile_kernel(TileArgs a) {
+  __shared__ __attribute__((aligned(1024))) char lds[5 * 256 * kStep * 2];
+  const TileWalk<256> walk(a.offsets, FORM == kGradient ? 0 : a.groups, a.rows, FORM == kGradient ? 1 : a.col_tiles);
+  run_tiles<T, FORM, 256, 256, 2, 4, false>(a, lds, walk);
+  if (FORM != kGradient) {
+    __syncthreads();
+    run_tiles<T, FORM, 128, 256, 2, 4, true>(a, lds, walk);
+    // rows behind the last group
+    typedef T Part __attribute__((ext_vector_type(8)));
     const GroupRange g = group_range(a.offsets, a.groups, a.rows, a.groups);
     const int parts = a.outc / 8;
     const int64_t pieces = (g.end - g.begin) * parts;
     Part q;
 #pragma unroll
     for (int u = 0; u < 8; ++u) q[u] = static_cast<T>(0.0f);
-    for (int64_t i = (int64_t)blockIdx.x * (NW * 64) + tid; i < pieces; i += (int64_t)gridDim.x * (NW * 64))
+    for (int64_t i = (int64_t)blockIdx.x * 512 + threadIdx.x; i < pieces; i += (int64_t)gridDim.x * 512)
       *reinterpret_cast<Part*>(static_cast<T*>(a.out) + (g.begin + i / parts) * a.ldo + i % parts * 8) = q;
   }
 }
@@ -855,14 +865,15 @@ hipError_t product_typed(const GroupedArgs& a, bool transpose, hipStream_t st) {
   if constexpr (sizeof(T) == 2) {
     if (tiled) {
       const int cols = (outc + 255) / 256;
-      const int64_t n = tile_bound(a.rows, a.groups, 256, cols);
+      const int64_t n = 2 * tile_bound(a.rows, a.groups, 256, cols);  // pieces of half a tile
+      const uint32_t grid = (uint32_t)(n < 256 ? n : 256);
       const TileArgs t{a.x, a.w, a.y, a.offsets, a.order, a.ldx, a.ldw, a.ldg, a.ldy, 0, a.rows, a.xrows,
                        (uint32_t)(((a.xrows - 1) * a.ldx + depth) * 2), (uint32_t)(((a.N - 1) * a.ldw + a.K) * 2),
                        a.groups, a.slots, 0, outc, depth, 0, cols, Parts{0, nullptr}};
       if (transpose)
-        grouped_tile_kernel<T, kTransposed, 256, 256, 2, 4><<<(uint32_t)(n < 256 ? n : 256), 512, 0, st>>>(t);
+        grouped_tile_kernel<T, kTransposed><<<grid, 512, 0, st>>>(t);
       else
-        grouped_tile_kernel<T, kProduct, 256, 256, 2, 4><<<(uint32_t)(n < 256 ? n : 256), 512, 0, st>>>(t);
+        grouped_tile_kernel<T, kProduct><<<grid, 512, 0, st>>>(t);
       return hipGetLastError();
     }
   }
@@ -932,10 +943,11 @@ hipError_t gradient_typed(const GradientArgs& a, hipStream_t st) {
     if (tiled && c.side == 256) {
       const int wr = (a.N + 255) / 256, wc = (a.K + 255) / 256;
       const int64_t n = (c.part ? c.parts : a.groups) * wr * wc;
+      const uint32_t grid = (uint32_t)(n < 256 ? n : 256);
       const TileArgs t{a.dy, a.x, a.dw, a.offsets, a.order, a.lddy, a.ldx, 0, a.ldw, a.ldg, a.rows, a.xrows,
                        (uint32_t)(((a.rows - 1) * a.lddy + a.N) * 2), (uint32_t)(((a.xrows - 1) * a.ldx + a.K) * 2),
                        a.groups, a.slots, a.N, a.K, 0, wr, wc, parts};
-      grouped_tile_kernel<T, kGradient, 256, 256, 2, 4><<<(uint32_t)(n < 256 ? n : 256), 512, 0, st>>>(t);
+      grouped_tile_kernel<T, kGradient><<<grid, 512, 0, st>>>(t);
       e = hipGetLastError();
       done = true;
     }

@@ -80,19 +80,21 @@ __device__ __forceinline__ RowTile find_tile(const int32_t* offsets, int groups,
   return t;
 }
 
-// The same for workgroups that take one tile after the other: this workgroup's tiles, 0 ... count - 1.  Each die (eight of them,
-// workgroups go to them in turn) has a contiguous eighth of all tiles, column tiles of a row tile side by side, and its workgroups
-// take them side by side: what they read at one time is shared in the die's L2.  (A group's last tile, which has fewer rows, takes
-// as long as a full one.  All of them at the end, or their missing rows left out of the products, was slower: 615 and 605 instead of
-// 590 us for 65,536 rows in 64 uneven groups, 2048 x 2048.)
+// The same for workgroups that take one tile after the other.  Each die (eight of them, workgroups go to them in turn) has a
+// contiguous eighth of all tiles, column tiles of a row tile side by side, and its workgroups take them side by side: what they read
+// at one time is shared in the die's L2.  Tiles 0 ... count - 1 are this workgroup's.  Where the tiles that would make a last
+// round are for at most half of the workgroups, they are cut in two along the rows, and half() is this workgroup's piece.
+// (A group's last tile, which has fewer rows, takes as long as a full one.  All of them at the end, or their missing rows left out
+// of the products, was slower: 615 and 605 instead of 590 us for 65,536 rows in 64 uneven groups, 2048 x 2048.)
 template <int BM>
 struct TileWalk {
   const int32_t* offsets;
   int64_t rows;
   int groups, per;
   int mine, sum;  // row tiles of this lane's groups; of those of the lanes up to it
-  int cols, stride;
-  int64_t first, count;
+  int cols, stride, side;
+  int64_t first, full, halves;  // of the die: its first tile, tiles that are taken whole, that are cut
+  int64_t count;
 
   __device__ __forceinline__ TileWalk(const int32_t* o, int g, int64_t r, int c) : offsets(o), rows(r), groups(g), cols(c) {
     const int lane = threadIdx.x & 63;
@@ -111,12 +113,26 @@ struct TileWalk {
     }
     const int64_t total = (int64_t)__builtin_amdgcn_readlane(sum, 63) * cols, share = (total + 7) / 8;
     stride = gridDim.x >> 3;
-    first = (int64_t)(blockIdx.x & 7) * share + (blockIdx.x >> 3);
-    const int64_t end = min(total, (int64_t)((blockIdx.x & 7) + 1) * share);
-    count = end > first ? (end - first + stride - 1) / stride : 0;
+    side = blockIdx.x >> 3;
+    first = min(total, (int64_t)(blockIdx.x & 7) * share);
+    full = min(total, first + share) - first;
+    halves = full % stride;
+    if (2 * halves > stride) halves = 0;
+    full -= halves;
+    count = full > side ? (full - side + stride - 1) / stride : 0;
   }
-  __device__ __forceinline__ RowTile at(int64_t i) const {
-    const int64_t index = first + i * stride;
+  __device__ __forceinline__ RowTile at(int64_t i) const { return tile(first + side + i * stride); }
+  __device__ __forceinline__ RowTile half() const {  // group -1: none
+    RowTile t;
+    t.group = -1;
+    if (side >= 2 * halves) return t;
+    t = tile(first + full + (side >> 1));
+    t.begin += (side & 1) * (BM / 2);
+    t.count = min(t.count - (side & 1) * (BM / 2), BM / 2);
+    if (t.count <= 0) t.group = -1;
+    return t;
+  }
+  __device__ __forceinline__ RowTile tile(int64_t index) const {
     const int row_tile = (int)(index / cols);
     const int owner = __ffsll((unsigned long long)__ballot(row_tile < sum)) - 1;
     int left = row_tile - __builtin_amdgcn_readlane(sum - mine, owner);
@@ -244,8 +260,12 @@ __device__ __forceinline__ void read_by_all() { asm volatile("s_waitcnt lgkmcnt(
 // Neighbouring results, of which `left` exist, to a place that may begin anywhere.
 template <typename T, int N>
 __device__ __forceinline__ void store_any(T* p, const T (&v)[N], int left) {
+  typedef T Whole __attribute__((ext_vector_type(N), aligned(sizeof(T))));
   if (left >= N) {
-    __builtin_memcpy(p, v, sizeof(v));
+    Whole w;
+#pragma unroll
+    for (int u = 0; u < N; ++u) w[u] = v[u];
+    *reinterpret_cast<Whole*>(p) = w;
   } else {
 #pragma unroll
     for (int u = 0; u < N; ++u)
