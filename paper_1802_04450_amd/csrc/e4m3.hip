@@ -517,7 +517,7 @@ __device__ __forceinline__ int fragment_col(int i) { return (i & 0x13) | ((i & 4
 // All tiles of BM rows of a workgroup, or (HALF) its one piece of half a tile.
 template <typename T, int BM, bool HALF>
 __device__ __forceinline__ void run_tiles(const E4m3Args& a, uint8_t* lds, const TileWalk<256>& walk) {
-  constexpr int BN = 256, WC = 4, NW = 8, FR = BM / 64, FC = 2, RLOADS = BM / 64, CLOADS = 4;
+  constexpr int BN = 256, WC = 4, FR = BM / 64, FC = 2, RLOADS = BM / 64, CLOADS = 4;
   constexpr int BUFFER = 256 * kScaleBlock;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);

@@ -54,6 +54,38 @@ __device__ __forceinline__ typename Matrix<T>::Chunk load_any(const T* p, int64_
   return v;
 }
 
+// 16 bytes from p on, which may begin anywhere, of a row that has `width` values there: all 16 bytes are in it, or p is where they begin.
+template <typename T>
+__device__ __forceinline__ typename Matrix<T>::Chunk load_whole(const T* p, int width) {
+  if (width >= Matrix<T>::kChunk) {  // the same for all
+    typename Matrix<T>::Chunk v;
+    __builtin_memcpy(&v, p, sizeof(v));
+    return v;
+  }
+  return load_any<T>(p, width);
+}
+// The values of v from the s-th on (up to all of them), and zeros.
+template <typename T>
+__device__ __forceinline__ typename Matrix<T>::Chunk shifted(typename Matrix<T>::Chunk v, int s) {
+  union {
+    typename Matrix<T>::Chunk c;
+    uint32_t d[4];
+  } x;
+  x.c = v;
+  const int bytes = s * (int)sizeof(T);
+  if (sizeof(T) == 2) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x.d[i] = bytes & 2 ? x.d[i] >> 16 | (i < 3 ? x.d[i + 1] << 16 : 0) : x.d[i];
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) x.d[i] = bytes & 4 ? (i < 3 ? x.d[i + 1] : 0) : x.d[i];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) x.d[i] = bytes & 8 ? (i < 2 ? x.d[i + 2] : 0) : x.d[i];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) x.d[i] = bytes & 16 ? 0 : x.d[i];
+  return x.c;
+}
+
 // ---- any strides, any alignment ------------------------------------------------------------------------------------------
 // out(r, c) = sum over e of R(r, e) C(c, e), a TILE x TILE tile of out by four waves, a quarter each.  The contraction goes through
 // two buffers of LDS in steps of 4 U chunks: the next step's chunks are loaded into registers while this one's products run.
@@ -65,13 +97,15 @@ typedef short short4v __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) short4v LdsShort4;
 
 // Where a part of a gradient's contraction goes: the rows of a group are cut into parts of `part` (0: not at all), whose sums in
-// fp32 lie one after the other in `sums`, groups x their parts x N x K.
+// fp32 lie one after the other in `sums`, groups x their parts x N x K.  There is room for `most` parts, as many as groups that do
+// not overlap can have.
 struct Parts {
   int part;
+  int64_t most;
   float* sums;
 };
 
-template <typename T, int FORM, int TILE, int U>
+template <typename T, int FORM, int TR, int TC, int U>
 __global__ __launch_bounds__(256) void grouped_any_kernel(const T* __restrict__ rmat, const T* __restrict__ cmat, T* __restrict__ out,
                                                           const int32_t* __restrict__ offsets, const int32_t* __restrict__ order,
                                                           int64_t ldr, int64_t ldc, int64_t ldg, int64_t ldo, int64_t ldog,
@@ -82,9 +116,9 @@ __global__ __launch_bounds__(256) void grouped_any_kernel(const T* __restrict__ 
   constexpr int BK = 4 * CH * U;
   constexpr bool R_ALONG = FORM != kGradient, C_ALONG = FORM == kProduct;
   // rows of a tile in LDS, so that the rows read at one time do not all begin in one bank
-  constexpr int ALONG = BK + CH, ACROSS = TILE + 2 * CH;
-  constexpr int RSIZE = R_ALONG ? TILE * ALONG : BK * ACROSS, CSIZE = C_ALONG ? TILE * ALONG : BK * ACROSS;
-  constexpr int LOADS = TILE * BK / CH / 256, F = TILE / 32;
+  constexpr int ALONG = BK + (U == 1 ? 2 : 1) * CH, PAD = sizeof(T) == 2 ? 2 * CH : CH, RACROSS = TR + PAD, CACROSS = TC + PAD;
+  constexpr int RSIZE = R_ALONG ? TR * ALONG : BK * RACROSS, CSIZE = C_ALONG ? TC * ALONG : BK * CACROSS;
+  constexpr int LR = TR * BK / CH / 256, LC = TC * BK / CH / 256, FR = TR / 32, FC = TC / 32;
   __shared__ __attribute__((aligned(16))) T lds[2][RSIZE + CSIZE];
   int group, r0 = 0, rn, c0;
   int64_t pbegin = 0, length;
@@ -92,9 +126,9 @@ __global__ __launch_bounds__(256) void grouped_any_kernel(const T* __restrict__ 
   if (FORM == kGradient) {
     const int per = row_tiles * col_tiles;
     const int index = blockIdx.x / per, in = blockIdx.x - index * per;
-    r0 = in / col_tiles * TILE;
-    c0 = in % col_tiles * TILE;
-    rn = min(TILE, outr - r0);
+    r0 = in / col_tiles * TR;
+    c0 = in % col_tiles * TC;
+    rn = min(TR, outr - r0);
     if (parts.part) {
       const RowTile t = part_at(offsets, groups, rows, parts.part, index);
       if (t.group < 0) return;
@@ -109,80 +143,115 @@ __global__ __launch_bounds__(256) void grouped_any_kernel(const T* __restrict__ 
       length = g.end - g.begin;
     }
   } else {
-    const RowTile t = find_tile<TILE>(offsets, groups, rows, col_tiles);
+    const RowTile t = find_tile<TR>(offsets, groups, rows, col_tiles);
     if (t.group < 0) return;
     group = t.group;
     pbegin = t.begin;
     rn = t.count;
-    c0 = t.col * TILE;
+    c0 = t.col * TC;
     length = group == groups ? 0 : depth;
   }
-  const int cn = min(TILE, outc - c0);
+  if (xrows == 0) length = 0;  // nothing but zeros
+  const int cn = min(TC, outc - c0);
   const T* cbase = FORM == kGradient || length == 0 ? cmat : cmat + (int64_t)group * ldg;
 
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   const int sub = lane & 15, quad = lane >> 4;
-  const int wr = (wave >> 1) * (TILE / 2), wc = (wave & 1) * (TILE / 2);
-  f32x4 acc[F][F];
+  const int wr = (wave >> 1) * (TR / 2), wc = (wave & 1) * (TC / 2);
+  f32x4 acc[FR][FC];
 #pragma unroll
-  for (int a = 0; a < F; ++a)
+  for (int a = 0; a < FR; ++a)
 #pragma unroll
-    for (int b = 0; b < F; ++b) acc[a][b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int b = 0; b < FC; ++b) acc[a][b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
-  // A thread's chunks, LOADS of each operand: chunk i is piece i % (BK / CH) of row i / (BK / CH), or, across, piece i % (TILE / CH) of
-  // step i / (TILE / CH).
+  // A thread's chunks, LR and LC of the operands: chunk i is piece i % (BK / CH) of row i / (BK / CH), or, across, piece i % (width / CH)
+  // of step i / (width / CH).  Every one is a whole 16-byte load from within its row: one that reaches beyond the row's end is moved back
+  // to end there, one of a row that does not exist takes another row's, and `skip` says how many of its values are
+  // not wanted (CH: none is).
   auto along_row = [&](int u) { return (tid + u * 256) / (BK / CH); };
   auto along_e = [&](int u) { return (tid + u * 256) % (BK / CH) * CH; };
-  auto across_e = [&](int u) { return (tid + u * 256) / (TILE / CH); };
-  auto across_col = [&](int u) { return (tid + u * 256) % (TILE / CH) * CH; };
-  const T *rp[LOADS], *cp[LOADS];
-  int look[LOADS];
+  auto across_e = [&](int u, int width) { return (tid + u * 256) / (width / CH); };
+  auto across_col = [&](int u, int width) { return (tid + u * 256) % (width / CH) * CH; };
+  const int rwidth = R_ALONG ? depth : outr - r0, cwidth = C_ALONG ? depth : outc - c0;
+  const T *rp[LR], *cp[LC];
+  int look[LC], rskip[LR], cskip[LC];  // `across` or a missing row: always
 #pragma unroll
-  for (int u = 0; u < LOADS; ++u) {
-    rp[u] = cp[u] = nullptr;  // nothing there
+  for (int u = 0; u < LR; ++u) {
     if (R_ALONG) {
       const int64_t src = along_row(u) < rn && length > 0 ? source_row(order, pbegin + along_row(u), slots, xrows) : -1;
-      if (src >= 0) rp[u] = rmat + src * ldr + along_e(u);
-    } else if (across_col(u) < rn) {
-      rp[u] = rmat + (pbegin + across_e(u)) * ldr + r0 + across_col(u);
+      rskip[u] = src < 0 ? CH : 0;
+      rp[u] = rmat + (src < 0 ? 0 : src) * ldr;
+    } else {
+      const int col = across_col(u, TR), from = max(min(col, rwidth - CH), 0);
+      rskip[u] = min(col - from, CH);
+      rp[u] = rmat + pbegin * ldr + r0 + from;
     }
+  }
+#pragma unroll
+  for (int u = 0; u < LC; ++u) {
     if (C_ALONG) {
-      if (along_row(u) < cn) cp[u] = cbase + (int64_t)(c0 + along_row(u)) * ldc + along_e(u);
-    } else if (across_col(u) < cn) {
-      cp[u] = cbase + (FORM == kGradient ? 0 : across_e(u) * ldc) + c0 + across_col(u);
+      cskip[u] = along_row(u) < cn ? 0 : CH;
+      cp[u] = cbase + (int64_t)(c0 + min(along_row(u), cn - 1)) * ldc;
+    } else {
+      const int col = across_col(u, TC), from = max(min(col, cwidth - CH), 0);
+      cskip[u] = min(col - from, CH);
+      cp[u] = cbase + c0 + from;
     }
   }
   auto look_up = [&](int64_t e0) {  // gradient: the rows of x that the next step takes
     if (FORM == kGradient) {
 #pragma unroll
-      for (int u = 0; u < LOADS; ++u) {
-        const int64_t e = e0 + across_e(u);
+      for (int u = 0; u < LC; ++u) {
+        const int64_t e = e0 + across_e(u, TC);
         look[u] = e < length ? (int)source_row(order, pbegin + e, slots, xrows) : -1;
       }
     }
   };
-  auto load = [&](int64_t e0, Chunk (&r)[LOADS], Chunk (&c)[LOADS]) {
+  Chunk r[LR], c[LC];
+  int rs[LR], cs[LC];
+  auto load = [&](int64_t e0) {
 #pragma unroll
-    for (int u = 0; u < LOADS; ++u) {
-      if (R_ALONG)
-        r[u] = load_any<T>(rp[u] + e0, rp[u] ? length - e0 - along_e(u) : 0);
-      else
-        r[u] = load_any<T>(rp[u] + e0 * ldr, rp[u] && e0 + across_e(u) < length ? rn - across_col(u) : 0);
-      if (C_ALONG)
-        c[u] = load_any<T>(cp[u] + e0, cp[u] ? length - e0 - along_e(u) : 0);
-      else if (FORM == kGradient)
-        c[u] = load_any<T>(cp[u] + (look[u] < 0 ? 0 : look[u]) * ldc, cp[u] && look[u] >= 0 ? cn - across_col(u) : 0);
-      else
-        c[u] = load_any<T>(cp[u] + e0 * ldc, cp[u] && e0 + across_e(u) < length ? cn - across_col(u) : 0);
+    for (int u = 0; u < LR; ++u) {
+      if (R_ALONG) {
+        const int64_t e = e0 + along_e(u), from = max(min(e, length - CH), (int64_t)0);
+        rs[u] = max(rskip[u], (int)min(e - from, (int64_t)CH));
+        r[u] = load_whole<T>(rp[u] + from, rwidth);
+      } else {
+        const int64_t e = e0 + across_e(u, TR);
+        rs[u] = e < length ? rskip[u] : CH;
+        r[u] = load_whole<T>(rp[u] + min(e, length - 1) * ldr, rwidth);
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < LC; ++u) {
+      if (C_ALONG) {
+        const int64_t e = e0 + along_e(u), from = max(min(e, length - CH), (int64_t)0);
+        cs[u] = max(cskip[u], (int)min(e - from, (int64_t)CH));
+        c[u] = load_whole<T>(cp[u] + from, cwidth);
+      } else if (FORM == kGradient) {
+        cs[u] = look[u] < 0 ? CH : cskip[u];
+        c[u] = load_whole<T>(cp[u] + (int64_t)max(look[u], 0) * ldc, cwidth);
+      } else {
+        const int64_t e = e0 + across_e(u, TC);
+        cs[u] = e < length ? cskip[u] : CH;
+        c[u] = load_whole<T>(cp[u] + min(e, length - 1) * ldc, cwidth);
+      }
     }
   };
-  auto put = [&](T* tile, bool along, const Chunk (&v)[LOADS]) {
+  auto put = [&](T* rt, T* ct) {
 #pragma unroll
-    for (int u = 0; u < LOADS; ++u)
-      *reinterpret_cast<Chunk*>(along ? tile + along_row(u) * ALONG + along_e(u) : tile + across_e(u) * ACROSS + across_col(u)) = v[u];
+    for (int u = 0; u < LR; ++u) {
+      if (__any(rs[u])) r[u] = shifted<T>(r[u], rs[u]);
+      *reinterpret_cast<Chunk*>(R_ALONG ? rt + along_row(u) * ALONG + along_e(u) : rt + across_e(u, TR) * RACROSS + across_col(u, TR)) = r[u];
+    }
+#pragma unroll
+    for (int u = 0; u < LC; ++u) {
+      if (__any(cs[u])) c[u] = shifted<T>(c[u], cs[u]);
+      *reinterpret_cast<Chunk*>(C_ALONG ? ct + along_row(u) * ALONG + along_e(u) : ct + across_e(u, TC) * CACROSS + across_col(u, TC)) = c[u];
+    }
   };
   // Rows (columns) first ... first + 15 of an operand, the kk-th 4 chunks of the step.
-  auto fragment = [&](const T* tile, bool along, int first, int kk) {
+  auto fragment = [&](const T* tile, bool along, int pitch, int first, int kk) {
     if (along) return *reinterpret_cast<const Chunk*>(tile + (first + sub) * ALONG + (kk * 4 + quad) * CH);
     const int e = (kk * 4 + quad) * CH;
     Chunk f;
@@ -193,56 +262,53 @@ __global__ __launch_bounds__(256) void grouped_any_kernel(const T* __restrict__ 
       } u;
 #pragma unroll
       for (int h = 0; h < 2; ++h)
-        u.half[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsShort4*)(tile + (e + h * 4 + (sub >> 2)) * ACROSS + first + (sub & 3) * 4));
+        u.half[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsShort4*)(tile + (e + h * 4 + (sub >> 2)) * pitch + first + (sub & 3) * 4));
       f = u.whole;
     } else {
 #pragma unroll
-      for (int j = 0; j < CH; ++j) f[j] = tile[(e + j) * ACROSS + first + sub];
+      for (int j = 0; j < CH; ++j) f[j] = tile[(e + j) * pitch + first + sub];
     }
     return f;
   };
 
-  Chunk r[LOADS], c[LOADS];
   if (length > 0) {
     look_up(0);
-    load(0, r, c);
+    load(0);
     look_up(BK);
   }
   int now = 0;
   for (int64_t e0 = 0; e0 < length; e0 += BK) {
     T* rt = lds[now];
     T* ct = lds[now] + RSIZE;
-    put(rt, R_ALONG, r);
-    put(ct, C_ALONG, c);
+    put(rt, ct);
     __syncthreads();  // the other buffer has been read by all by then
     if (e0 + BK < length) {
-      load(e0 + BK, r, c);
+      load(e0 + BK);
       look_up(e0 + 2 * BK);
     }
 #pragma unroll
     for (int kk = 0; kk < U; ++kk) {
-      Chunk fr[F], fc[F];
+      Chunk fr[FR], fc[FC];
 #pragma unroll
-      for (int a = 0; a < F; ++a) {
-        fr[a] = fragment(rt, R_ALONG, wr + a * 16, kk);
-        fc[a] = fragment(ct, C_ALONG, wc + a * 16, kk);
-      }
+      for (int a = 0; a < FR; ++a) fr[a] = fragment(rt, R_ALONG, RACROSS, wr + a * 16, kk);
 #pragma unroll
-      for (int a = 0; a < F; ++a)
+      for (int b = 0; b < FC; ++b) fc[b] = fragment(ct, C_ALONG, CACROSS, wc + b * 16, kk);
 #pragma unroll
-        for (int b = 0; b < F; ++b) acc[a][b] = Matrix<T>::mma(fc[b], fr[a], acc[a][b]);  // a lane gets four neighbours of a row
+      for (int a = 0; a < FR; ++a)
+#pragma unroll
+        for (int b = 0; b < FC; ++b) acc[a][b] = Matrix<T>::mma(fc[b], fr[a], acc[a][b]);  // a lane gets four neighbours of a row
     }
     now ^= 1;
   }
 
   T* obase = FORM == kGradient ? out + (int64_t)group * ldog : out;
 #pragma unroll
-  for (int a = 0; a < F; ++a) {
+  for (int a = 0; a < FR; ++a) {
     const int row = wr + a * 16 + sub;
     if (row >= rn) continue;
     T* orow = obase + ((FORM == kGradient ? (int64_t)r0 : pbegin) + row) * ldo + c0;
 #pragma unroll
-    for (int b = 0; b < F; ++b) {
+    for (int b = 0; b < FC; ++b) {
       const int col = wc + b * 16 + quad * 4;
       if (col >= cn) continue;
       if (FORM == kGradient && sums) {
@@ -267,6 +333,7 @@ __global__ __launch_bounds__(256) void gradient_sum_kernel(Parts parts, const in
   const int64_t size = (int64_t)N * K;
   int first, count;
   parts_of(offsets, groups, rows, parts.part, g, first, count);
+  if (first + count > parts.most) count = max(0, (int)parts.most - first);
   const float* sums = parts.sums + first * size;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < size; i += (int64_t)gridDim.x * 256) {
     float sum = 0.0f;
@@ -433,7 +500,7 @@ __device__ __forceinline__ void run_tiles(const TileArgs& a, char* lds, const Ti
   const GroupOrder by_length(a.offsets, FORM == kGradient && !a.parts.part ? a.groups : 0, a.rows);
   const PartList part_list(a.offsets, FORM == kGradient && a.parts.part ? a.groups : 0, a.rows, a.parts.part);
   const int per_group = a.row_tiles * a.col_tiles;  // gradient
-  const int64_t group_parts = FORM != kGradient ? 0 : a.parts.part ? part_list.total : a.groups;
+  const int64_t group_parts = FORM != kGradient ? 0 : a.parts.part ? min((int64_t)part_list.total, a.parts.most) : a.groups;
   // A gradient's tiles take as long as their groups are.  From the longest group to the shortest they are dealt out to all
   // workgroups, to and fro.
   const int64_t count = FORM == kGradient ? (group_parts * per_group + gridDim.x - 1) / gridDim.x : HALF ? 1 : walk.count;
@@ -831,16 +898,19 @@ hipError_t thin_typed(const GroupedArgs& a, hipStream_t st) {
 bool short_offsets(int64_t rows, int64_t ld) { return rows > 0 && (rows + 3 * kStep) * ld * 2 < (int64_t)0xf0000000; }
 
 // Tiles of a general kernel: 128 x 128 where there are enough of them, else 64 x 64.
-bool large_tiles(int64_t row_tiles_128, int64_t cols, int row_parts = 1) { return row_tiles_128 * ((cols + 127) / 128) * row_parts >= 512; }
+bool large_tiles(int64_t row_tiles_128, int64_t cols) { return row_tiles_128 * ((cols + 127) / 128) >= 512; }
 
 template <typename T, int FORM, int TILE>
 hipError_t any_typed(const GroupedArgs& a, int outc, int depth, hipStream_t st) {
+  // In 32 bits rows of tiles are half as high: a tile takes long, and few more than the chip holds leave much of it idle at the end
+  // (65,536 rows, 8 groups of 256 x 256 101 -> 87 us; in 16 bits 16,384 rows, 16 groups of 777 x 1,001 82 -> 94).
+  constexpr int TR = TILE == 128 && sizeof(T) == 4 ? 64 : TILE;
   const int cols = (outc + TILE - 1) / TILE;
-  const int64_t blocks = tile_bound(a.rows, a.groups, TILE, cols);
+  const int64_t blocks = tile_bound(a.rows, a.groups, TR, cols);
   if (blocks > 0x7fffffff) return hipErrorInvalidConfiguration;
-  grouped_any_kernel<T, FORM, TILE, TILE == 64 ? 2 : 1><<<(uint32_t)blocks, 256, 0, st>>>(
+  grouped_any_kernel<T, FORM, TR, TILE, TILE == 64 ? 2 : 1><<<(uint32_t)blocks, 256, 0, st>>>(
       static_cast<const T*>(a.x), static_cast<const T*>(a.w), static_cast<T*>(a.y), a.offsets, a.order, a.ldx, a.ldw, a.ldg, a.ldy, 0,
-      a.rows, a.xrows, a.groups, a.slots, 0, outc, depth, 0, cols, Parts{0, nullptr});
+      a.rows, a.xrows, a.groups, a.slots, 0, outc, depth, 0, cols, Parts{0, 0, nullptr});
   return hipGetLastError();
 }
 
@@ -869,7 +939,7 @@ hipError_t product_typed(const GroupedArgs& a, bool transpose, hipStream_t st) {
       const uint32_t grid = (uint32_t)(n < 256 ? n : 256);
       const TileArgs t{a.x, a.w, a.y, a.offsets, a.order, a.ldx, a.ldw, a.ldg, a.ldy, 0, a.rows, a.xrows,
                        (uint32_t)(((a.xrows - 1) * a.ldx + depth) * 2), (uint32_t)(((a.N - 1) * a.ldw + a.K) * 2),
-                       a.groups, a.slots, 0, outc, depth, 0, cols, Parts{0, nullptr}};
+                       a.groups, a.slots, 0, outc, depth, 0, cols, Parts{0, 0, nullptr}};
       if (transpose)
         grouped_tile_kernel<T, kTransposed><<<grid, 512, 0, st>>>(t);
       else
@@ -896,10 +966,12 @@ GradientCut gradient_cut(int64_t rows, int groups, int N, int K, int dtype) {
   const bool tiled = dtype != kF32 && N % 8 == 0 && K % 8 == 0;
   const int64_t small = (int64_t)((N + 63) / 64) * ((K + 63) / 64), large = (int64_t)((N + 127) / 128) * ((K + 127) / 128),
                 huge = (int64_t)((N + 255) / 256) * ((K + 255) / 256);
-  // 256 x 256 tiles want rows enough for all workgroups to have some steps; else the smaller the more workgroups
+  // 256 x 256 tiles want rows enough for all workgroups to have some steps; else the smaller the more workgroups.  128 x 128 where
+  // they cover no more than 64 x 64 would read the rows half as often, and half the workgroups do (100,003 rows, 100 groups of
+  // 100 x 90 in 16 bits 26 us, with 64 x 64 37; in 32 bits 62 and 67; of 64 x 90, where they cover twice as much, 58 and 37).
   if (tiled && huge * (rows / 512 + groups) >= 128)
     c.side = 256, c.tiles = huge;
-  else if (large * (rows / 512 + groups) >= 512)
+  else if (large * (rows / 512 + groups) >= (4 * large <= small ? 256 : 512))
     c.side = 128, c.tiles = large;
   else
     c.side = 64, c.tiles = small;
@@ -922,7 +994,7 @@ hipError_t any_gradient(const GradientArgs& a, const GradientCut& c, const Parts
   const int rt = (a.N + TILE - 1) / TILE, ct = (a.K + TILE - 1) / TILE;
   const int64_t blocks = (c.part ? c.parts : a.groups) * rt * ct;
   if (blocks > 0x7fffffff) return hipErrorInvalidConfiguration;
-  grouped_any_kernel<T, kGradient, TILE, TILE == 64 ? 2 : 1><<<(uint32_t)blocks, 256, 0, st>>>(
+  grouped_any_kernel<T, kGradient, TILE, TILE, TILE == 64 ? 2 : 1><<<(uint32_t)blocks, 256, 0, st>>>(
       static_cast<const T*>(a.dy), static_cast<const T*>(a.x), static_cast<T*>(a.dw), a.offsets, a.order, a.lddy, a.ldx, 0, a.ldw,
       a.ldg, a.rows, a.xrows, a.groups, a.slots, a.N, a.K, 0, rt, ct, parts);
   return hipGetLastError();
@@ -933,7 +1005,7 @@ hipError_t gradient_typed(const GradientArgs& a, hipStream_t st) {
   constexpr int CH = Matrix<T>::kChunk;
   GradientCut c = gradient_cut(a.rows, a.groups, a.N, a.K, a.dtype);
   if (c.part && !a.work) c.part = 0;
-  const Parts parts{c.part, c.part ? static_cast<float*>(a.work) : nullptr};
+  const Parts parts{c.part, c.parts, c.part ? static_cast<float*>(a.work) : nullptr};
   const bool tiled = sizeof(T) == 2 && whole_chunks<T>(a.x, a.ldx) && whole_chunks<T>(a.dy, a.lddy) && a.K % CH == 0 &&
                      a.N % CH == 0 && whole_chunks<T>(a.dw, a.ldw) && a.ldg % CH == 0 && short_offsets(a.rows, a.lddy) &&
                      short_offsets(a.xrows, a.ldx);

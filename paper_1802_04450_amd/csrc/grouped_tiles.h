@@ -21,6 +21,10 @@ __device__ __forceinline__ GroupRange group_range(const int32_t* offsets, int gr
   return r;
 }
 
+// Where groups overlap, which those of a routing do not, there may be any number of tiles: they are counted up to here, four times as
+// many as 2^31 rows make.
+constexpr int kMostTiles = 1 << 29;
+
 struct RowTile {
   int group;      // -1: none
   int64_t begin;  // first row of y
@@ -40,13 +44,13 @@ __device__ __forceinline__ RowTile find_tile(const int32_t* offsets, int groups,
   for (int u = 0; u < per; ++u) {
     if (g0 + u > groups) break;
     const GroupRange r = group_range(offsets, groups, rows, g0 + u);
-    mine += (int)((r.end - r.begin + BM - 1) / BM);
+    mine = min(mine + (int)((r.end - r.begin + BM - 1) / BM), kMostTiles);
   }
   int sum = mine;
 #pragma unroll
   for (int s = 1; s < 64; s <<= 1) {
     const int o = __shfl_up(sum, s);
-    if (lane >= s) sum += o;
+    if (lane >= s) sum = min(sum + o, kMostTiles);
   }
   RowTile t;
   t.group = -1;
@@ -103,13 +107,13 @@ struct TileWalk {
     for (int u = 0; u < per; ++u) {
       if (lane * per + u >= groups) break;
       const GroupRange range = group_range(offsets, groups, rows, lane * per + u);
-      mine += (int)((range.end - range.begin + BM - 1) / BM);
+      mine = min(mine + (int)((range.end - range.begin + BM - 1) / BM), kMostTiles);
     }
     sum = mine;
 #pragma unroll
     for (int s = 1; s < 64; s <<= 1) {
       const int v = __shfl_up(sum, s);
-      if (lane >= s) sum += v;
+      if (lane >= s) sum = min(sum + v, kMostTiles);
     }
     const int64_t total = (int64_t)__builtin_amdgcn_readlane(sum, 63) * cols, share = (total + 7) / 8;
     stride = gridDim.x >> 3;
@@ -171,13 +175,13 @@ struct PartList {
     for (int u = 0; u < per; ++u) {
       if (lane * per + u >= groups) break;
       const GroupRange range = group_range(offsets, groups, rows, lane * per + u);
-      mine += (int)((range.end - range.begin + part - 1) / part);
+      mine = min(mine + (int)((range.end - range.begin + part - 1) / part), kMostTiles);
     }
     sum = mine;
 #pragma unroll
     for (int s = 1; s < 64; s <<= 1) {
       const int v = __shfl_up(sum, s);
-      if (lane >= s) sum += v;
+      if (lane >= s) sum = min(sum + v, kMostTiles);
     }
     total = __builtin_amdgcn_readlane(sum, 63);
   }
