@@ -505,6 +505,7 @@ __global__ __launch_bounds__(KS > 4 ? KS * 64 : 256) void e4m3_thin_kernel(E4m3A
 // row hands over the same power of two.  Those come four steps at a time as one word a row, shifted by a byte a step.
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
+#ifdef __HIP_DEVICE_COMPILE__
 // How the 16-byte pieces of row r (column c) change places: a read takes 128 bytes of eight lanes and of the eight sixteen lanes
 // further at once, which then lie in different banks.
 __device__ __forceinline__ int row_shift(int r) { return (r & 6) | ((r >> 4) & 1); }
@@ -513,7 +514,6 @@ __device__ __forceinline__ int col_shift(int c) { return (c & 2) | ((c >> 1) & 4
 // four are eight neighbours.
 __device__ __forceinline__ int fragment_col(int i) { return (i & 0x13) | ((i & 4) << 1) | ((i & 8) >> 1); }
 
-#ifdef __HIP_DEVICE_COMPILE__
 // All tiles of BM rows of a workgroup, or (HALF) its one piece of half a tile.
 template <typename T, int BM, bool HALF>
 __device__ __forceinline__ void run_tiles(const E4m3Args& a, uint8_t* lds, const TileWalk<256>& walk) {
@@ -795,23 +795,34 @@ hipError_t quantize_typed(const T* x, int64_t ldx, int64_t rows, int K, uint8_t*
                           hipStream_t st) {
   constexpr int E = 16 / (int)sizeof(T);
   const int blocks_row = (K + kScaleBlock - 1) / kScaleBlock;
-  const int64_t grid = (rows * blocks_row + 15) / 16;
-  if (grid > 0x7fffffff) return hipErrorInvalidConfiguration;
-  if (reinterpret_cast<uintptr_t>(x) % 16 == 0 && ldx % E == 0 && K % E == 0)
-    quantize_kernel<T, true><<<(uint32_t)grid, 256, 0, st>>>(x, ldx, rows, K, blocks_row, q, ldq, scale, lds);
-  else
-    quantize_kernel<T, false><<<(uint32_t)grid, 256, 0, st>>>(x, ldx, rows, K, blocks_row, q, ldq, scale, lds);
-  return hipGetLastError();
+  const int64_t most = kMostThreads / 16 / blocks_row;  // rows a launch
+  const bool wide = reinterpret_cast<uintptr_t>(x) % 16 == 0 && ldx % E == 0 && K % E == 0;
+  for (int64_t r0 = 0; r0 < rows; r0 += most) {
+    const int64_t some = rows - r0 < most ? rows - r0 : most;
+    const uint32_t grid = (uint32_t)((some * blocks_row + 15) / 16);
+    if (wide)
+      quantize_kernel<T, true><<<grid, 256, 0, st>>>(x + r0 * ldx, ldx, some, K, blocks_row, q + r0 * ldq, ldq, scale + r0 * lds, lds);
+    else
+      quantize_kernel<T, false><<<grid, 256, 0, st>>>(x + r0 * ldx, ldx, some, K, blocks_row, q + r0 * ldq, ldq, scale + r0 * lds, lds);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 template <typename T>
 hipError_t dequantize_typed(const uint8_t* q, int64_t ldq, const uint8_t* scale, int64_t lds, int64_t rows, int K, T* x, int64_t ldx,
                             hipStream_t st) {
   const int parts = (K + 7) / 8;
-  const int64_t grid = (rows * parts + 255) / 256;
-  if (grid > 0x7fffffff) return hipErrorInvalidConfiguration;
-  dequantize_kernel<T><<<(uint32_t)grid, 256, 0, st>>>(q, ldq, scale, lds, rows, K, parts, x, ldx);
-  return hipGetLastError();
+  const int64_t most = kMostThreads / parts;  // rows a launch
+  for (int64_t r0 = 0; r0 < rows; r0 += most) {
+    const int64_t some = rows - r0 < most ? rows - r0 : most;
+    dequantize_kernel<T><<<(uint32_t)((some * parts + 255) / 256), 256, 0, st>>>(q + r0 * ldq, ldq, scale + r0 * lds, lds, some, K, parts,
+                                                                                x + r0 * ldx, ldx);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 template <typename T, int RF>

@@ -12,8 +12,7 @@ enum { kF32 = 0, kBF16 = 1, kF16 = 2 };  // SC_F32, SC_BF16, SC_F16
 constexpr int kMaxRouteClusters = 4096;
 constexpr int kMaxRouteChoices = 16;
 constexpr int kScaleBlock = 128;  // values that share a scale in the 8-bit form
-
-inline size_t type_bytes(int dtype) { return dtype == kF32 ? 4 : 2; }
+constexpr int64_t kMostThreads = 1 << 30;  // of one launch, which may not have 2^32
 
 // ---- route.hip ------------------------------------------------------------------------------------------------------
 size_t route_workspace(int64_t n, int k, int t);

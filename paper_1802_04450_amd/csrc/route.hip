@@ -517,14 +517,21 @@ hipError_t route_backward_typed(const T* scores, int64_t ld, const uint8_t* allo
   const bool wide = k % E == 0 && ld % E == 0 && ldd % E == 0 && reinterpret_cast<uintptr_t>(scores) % (E * sizeof(T)) == 0 &&
                     reinterpret_cast<uintptr_t>(ds) % (E * sizeof(T)) == 0 &&
                     (!allowed || (lda % E == 0 && reinterpret_cast<uintptr_t>(allowed) % E == 0));
-  const int64_t blocks = (n + kThreads / LANES - 1) / (kThreads / LANES);
-  if (wide)
-    route_backward_kernel<T, LANES, VPL, true><<<(uint32_t)blocks, kThreads, 0, st>>>(scores, ld, allowed, lda, n, k, t, normalize,
-                                                                                     idx, weight, dweight, ds, ldd);
-  else
-    route_backward_kernel<T, LANES, VPL, false><<<(uint32_t)blocks, kThreads, 0, st>>>(scores, ld, allowed, lda, n, k, t,
-                                                                                      normalize, idx, weight, dweight, ds, ldd);
-  return hipGetLastError();
+  for (int64_t i0 = 0; i0 < n; i0 += kMostThreads / LANES) {
+    const int64_t rows = n - i0 < kMostThreads / LANES ? n - i0 : kMostThreads / LANES;
+    const uint32_t blocks = (uint32_t)((rows + kThreads / LANES - 1) / (kThreads / LANES));
+    const T* s = scores ? scores + i0 * ld : nullptr;
+    const uint8_t* may = allowed ? allowed + i0 * lda : nullptr;
+    if (wide)
+      route_backward_kernel<T, LANES, VPL, true><<<blocks, kThreads, 0, st>>>(s, ld, may, lda, rows, k, t, normalize, idx + i0 * t,
+                                                                             weight + i0 * t, dweight + i0 * t, ds + i0 * ldd, ldd);
+    else
+      route_backward_kernel<T, LANES, VPL, false><<<blocks, kThreads, 0, st>>>(s, ld, may, lda, rows, k, t, normalize, idx + i0 * t,
+                                                                              weight + i0 * t, dweight + i0 * t, ds + i0 * ldd, ldd);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 template <typename T>
@@ -598,9 +605,10 @@ template <typename T, int E>
 __global__ __launch_bounds__(kThreads) void combine_backward_kernel(const T* __restrict__ dout, int64_t ldo, const T* __restrict__ z,
                                                                     int64_t ldz, int64_t rows, const int32_t* __restrict__ place,
                                                                     const float* __restrict__ weight,
-                                                                    const int32_t* __restrict__ order, int64_t slots, int t, int d,
-                                                                    T* __restrict__ dz, int64_t lddz, float* __restrict__ dweight) {
-  const int64_t q = (int64_t)blockIdx.x * (kThreads / kWave) + threadIdx.x / kWave;
+                                                                    const int32_t* __restrict__ order, int64_t q0, int64_t slots, int t,
+                                                                    int d, T* __restrict__ dz, int64_t lddz,
+                                                                    float* __restrict__ dweight) {
+  const int64_t q = q0 + (int64_t)blockIdx.x * (kThreads / kWave) + threadIdx.x / kWave;
   const int lane = threadIdx.x & (kWave - 1);
   if (q < slots) {
     const int32_t p = place[q];
@@ -645,12 +653,19 @@ hipError_t combine_typed(const T* z, int64_t ldz, int64_t rows, const int32_t* p
   constexpr int E = 16 / (int)sizeof(T);
   const bool wide = d % E == 0 && wide_rows<T>(z, ldz) && wide_rows<T>(out, ldo);
   const int parts = wide ? d / E : d;
-  const int64_t blocks = (n * parts + kThreads - 1) / kThreads;
-  if (wide)
-    combine_kernel<T, E><<<(uint32_t)blocks, kThreads, 0, st>>>(z, ldz, rows, place, weight, n, t, parts, out, ldo);
-  else
-    combine_kernel<T, 1><<<(uint32_t)blocks, kThreads, 0, st>>>(z, ldz, rows, place, weight, n, t, parts, out, ldo);
-  return hipGetLastError();
+  const int64_t most = parts < kMostThreads ? kMostThreads / parts : 1;  // rows a launch
+  for (int64_t i0 = 0; i0 < n; i0 += most) {
+    const int64_t some = n - i0 < most ? n - i0 : most;
+    const uint32_t blocks = (uint32_t)((some * parts + kThreads - 1) / kThreads);
+    const float* w = weight ? weight + i0 * t : nullptr;
+    if (wide)
+      combine_kernel<T, E><<<blocks, kThreads, 0, st>>>(z, ldz, rows, place + i0 * t, w, some, t, parts, out + i0 * ldo, ldo);
+    else
+      combine_kernel<T, 1><<<blocks, kThreads, 0, st>>>(z, ldz, rows, place + i0 * t, w, some, t, parts, out + i0 * ldo, ldo);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 template <typename T>
@@ -659,15 +674,20 @@ hipError_t combine_backward_typed(const T* dout, int64_t ldo, const T* z, int64_
                                   float* dweight, hipStream_t st) {
   constexpr int E = 16 / (int)sizeof(T);
   const int64_t slots = n * t, waves = slots > rows ? slots : rows;
-  const uint32_t blocks = (uint32_t)((waves + kThreads / kWave - 1) / (kThreads / kWave));
   const bool wide = d % E == 0 && wide_rows<T>(dout, ldo) && wide_rows<T>(dz, lddz) && (!dweight || wide_rows<T>(z, ldz));
-  if (wide)
-    combine_backward_kernel<T, E><<<blocks, kThreads, 0, st>>>(dout, ldo, z, ldz, rows, place, weight, order, slots, t, d, dz,
-                                                               lddz, dweight);
-  else
-    combine_backward_kernel<T, 1><<<blocks, kThreads, 0, st>>>(dout, ldo, z, ldz, rows, place, weight, order, slots, t, d, dz,
-                                                               lddz, dweight);
-  return hipGetLastError();
+  for (int64_t q0 = 0; q0 < waves; q0 += kMostThreads / kWave) {
+    const int64_t some = waves - q0 < kMostThreads / kWave ? waves - q0 : kMostThreads / kWave;
+    const uint32_t blocks = (uint32_t)((some + kThreads / kWave - 1) / (kThreads / kWave));
+    if (wide)
+      combine_backward_kernel<T, E><<<blocks, kThreads, 0, st>>>(dout, ldo, z, ldz, rows, place, weight, order, q0, slots, t, d, dz,
+                                                                 lddz, dweight);
+    else
+      combine_backward_kernel<T, 1><<<blocks, kThreads, 0, st>>>(dout, ldo, z, ldz, rows, place, weight, order, q0, slots, t, d, dz,
+                                                                 lddz, dweight);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 }  // namespace

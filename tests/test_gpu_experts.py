@@ -284,6 +284,79 @@ def test_grouped_product_offsets_beyond_32_bits(B):
     assert not bool(w[:-1].any())
 
 
+@pytest.mark.parametrize("rows,groups,N,K,kind", [(4096, 64, 64, 64, "f32"), (32768, 64, 256, 256, "bf16")])
+def test_grouped_gradient_overlapping_groups_stay_inside_the_workspace(B, rows, groups, N, K, kind):
+    """Groups that overlap have more parts than the workspace is made for."""
+    import ctypes
+    dev = torch.device(DEV)
+    dy, x = torch.ones(rows, N, dtype=TYPES[kind], device=DEV), torch.ones(rows, K, dtype=TYPES[kind], device=DEV)
+    offsets = torch.tensor([0, rows] * (groups // 2) + [0], dtype=torch.int32, device=DEV)
+    need = ctypes.c_size_t(0)
+    assert B.lib().sc_grouped_gradient_workspace_bytes(rows, groups, N, K, B._dtype(dy.dtype), ctypes.byref(need)) == B.SC_OK
+    assert 0 < need.value < 4 * N * K * (groups // 2) * (rows // 128)
+    work = torch.full((need.value + (64 << 20),), 77, dtype=torch.uint8, device=DEV)
+    out = torch.empty(groups, N, K, dtype=TYPES[kind], device=DEV)
+    B._enqueue(dev, B.lib().sc_grouped_gradient, B._ptr(dy), B._ld(dy), B._ptr(x), B._ld(x), rows, B._dtype(dy.dtype), B._ptr(offsets),
+               None, 1, rows, groups, N, K, B._ptr(out), B._ld(out, 1), B._ld(out), B._ptr(work), need.value)
+    assert bool((work[need.value:] == 77).all())
+    assert bool((out[0] == rows).all())                                    # the first group's parts are there
+
+
+# ---- more threads than one launch takes ---------------------------------------------------------------------------------
+def test_combine_more_threads_than_a_launch_takes(B):
+    """One thread a value: 2^32 of them, and more slots than 2^32 / 64."""
+    n, d, zs = 70_000_001, 65, 1000                                        # rows of 65 values of 16 bits: no whole 16 bytes
+    z = torch.randn(zs, d, device=DEV).bfloat16()
+    place = (torch.arange(n, device=DEV) % zs).int().view(n, 1)
+    out = B.sc_group_combine(z, place)
+    for at in (0, n // 4, n - zs):
+        i = torch.arange(at, at + zs, device=DEV)
+        assert torch.equal(out[i], z[i % zs])
+    order = torch.full((n,), 0, dtype=torch.int32, device=DEV)
+    order[-3:] = -1
+    place = torch.arange(n, dtype=torch.int32, device=DEV).view(n, 1)
+    place[-3:] = -1
+    dz, dw = B.sc_group_combine_backward(out, out, place, torch.full((n, 1), 2.0, device=DEV), order)
+    for at in (0, n // 4, n - zs):
+        i = torch.arange(at, at + zs, device=DEV)
+        ref = 2.0 * out[i].float()
+        ref[i >= n - 3] = 0.0
+        assert torch.equal(dz[i].float(), ref)
+        size = (out[i].float() ** 2).sum(1)
+        size[i >= n - 3] = 0.0
+        assert torch.allclose(dw[i, 0], size, rtol=(d + 8) * 2.0 ** -23, atol=0.0)
+
+
+def test_route_backward_more_threads_than_a_launch_takes(B):
+    n, k = 67_200_001, 129                                                 # 64 lanes a row
+    idx = (torch.arange(n, device=DEV) % k).int().view(n, 1)
+    dw = torch.ones(n, 1, device=DEV)
+    weight = torch.full((n, 1), 1.0 / k, device=DEV)
+    base = torch.zeros(n, k, dtype=torch.bfloat16, device=DEV)
+    ds = B.sc_route_backward(base, idx, weight, dw, normalize=False)
+    for at in (0, (1 << 24) - 7, 1 << 26, n - 500):
+        i = torch.arange(at, at + 500, device=DEV)
+        ref = torch.full((500, k), -1.0 / k / k, dtype=torch.float64, device=DEV)
+        ref[torch.arange(500, device=DEV), i % k] += 1.0 / k
+        assert torch.allclose(ds[i].double(), ref, rtol=2.0 ** -8, atol=1e-9)
+
+
+def test_blocks_more_threads_than_a_launch_takes(B):
+    rows, K, some = 67_200_001, 128, 1001                                  # 16 threads a row
+    few = torch.randn(some, K, device=DEV).bfloat16()
+    x = torch.empty(rows, K, dtype=torch.bfloat16, device=DEV)
+    for at in range(0, rows, some * 1024):
+        part = x[at:at + some * 1024]
+        part.copy_(few.repeat(1024, 1)[:part.shape[0]])
+    q, scale = B.sc_quantize_blocks(x)
+    fq, fs = B.sc_quantize_blocks(few)
+    back, fb = B.sc_dequantize_blocks(q, scale, K, torch.bfloat16), B.sc_dequantize_blocks(fq, fs, K, torch.bfloat16)
+    for at in (0, some * 30000, some * 67000, rows - rows % some):
+        m = min(some, rows - at)
+        assert torch.equal(q[at:at + m].view(torch.uint8), fq[:m].view(torch.uint8))
+        assert torch.equal(scale[at:at + m], fs[:m]) and torch.equal(back[at:at + m], fb[:m])
+
+
 # ---- weighted sum -----------------------------------------------------------------------------------------------------
 @pytest.mark.parametrize("n,t,d,dropped", [(1, 1, 1, 0.0), (16, 4, 2048, 0.0), (77, 3, 100, 0.3), (130, 8, 129, 0.1), (1000, 2, 64, 0.0),
                                            (40, 1, 4096, 0.5), (9, 16, 40, 1.0)])
