@@ -91,6 +91,11 @@ __device__ __forceinline__ typename Matrix<T>::Chunk shifted(typename Matrix<T>:
 // two buffers of LDS in steps of 4 U chunks: the next step's chunks are loaded into registers while this one's products run.
 // An operand whose rows run along the contraction lies in LDS row by row; one whose rows run across it step by step, and the
 // values of a fragment are put together when they are read (16 bits: by the transposing read).
+//
+// A step's loads and address sums take about as long as its products do, in turn: 16,384 rows of 777, 16 groups x 1,001 in 16 bits
+// 83 us, 307 TFLOP/s, in 32 bits 314 us, 81 TFLOP/s of the 154 that its matrix instructions reach; 100,003 rows of 90, 100 groups x
+// 100 in 32 bits 39 us, of which the matrix instructions are busy for 17, much of it for what fills the tiles up.  Two steps of
+// loads ahead instead of one 185 us for that product and its gradients, not 174; fragments that have no column left out 180.
 enum { kProduct = 0, kTransposed = 1, kGradient = 2 };
 
 typedef short short4v __attribute__((ext_vector_type(4)));
@@ -347,6 +352,7 @@ __global__ __launch_bounds__(256) void gradient_sum_kernel(Parts parts, const in
 // bounds it.  A wave has 16 columns and RF * 16 rows; KS of a workgroup's four waves share the columns, each with every KS-th
 // run of RUN chunks of the contraction, and their sums are added in order at the end: as few columns as there are, enough
 // waves are at work.  A run of the matrix is on its way while one is used.  Rows of any alignment: a lane's 16 bytes may begin anywhere.
+// 64 rows, 64 groups of 1024 x 2048 in 16 bits (268 MB) 53 us, 5.0 TB/s; 1 row of 2048 x 2048 6.4 us.
 constexpr int kThinRun = 4;
 
 template <typename T, int RF, int KS>
@@ -435,6 +441,11 @@ __global__ __launch_bounds__(KS > 4 ? KS * 64 : 256) void grouped_thin_kernel(Gr
 // Workgroups take one tile after the other: while the last two steps of a tile run, the first two of the next are fetched, and a
 // tile's results are stored while the next one's products run.  For that every tile has at least two steps, a gradient's three, as
 // the rows of x that a step takes are looked up a step before they are fetched; steps behind the contraction's end hold zeros.
+//
+// 65,536 rows, 64 groups of 2048 x 2048 in 16 bits: product and transposed 465 us (1,180 TFLOP/s), gradient 612 (900, its operands
+// both turned on the way out of LDS).  What bounds it is the matrix instructions' rate at the power they take: on operands of zeros
+// the same product takes a quarter less.  Four waves with 128 x 128 each read LDS less often, but spill or move registers to
+// and fro; 32 x 32 instructions, wave priorities and all tiles of 128 rows were no faster.
 constexpr int kStep = 64;
 constexpr uint32_t kNowhere = 0xfffffff0u;  // an offset behind every buffer's end: reads as zeros
 
@@ -873,10 +884,11 @@ template <typename T, int RF>
 hipError_t thin_typed(const GroupedArgs& a, hipStream_t st) {
   const int tiles = (a.N + 15) / 16;
   const int64_t met = a.rows < a.groups ? a.rows : a.groups;  // groups with rows, at most
-  // some 5,000 waves at work, few more than the chip holds at a time (64 rows, 64 groups of 1024 x 2048: one wave for its columns 59 us,
-  // two 46, four 48; 1 row of 2048 x 2048: four 10.8, sixteen ...)
+  // Waves enough to fill the chip, and no more (rows = groups, of 1024 x 2048 in 16 bits, one, two, four and eight waves for their
+  // columns: 64 53, 58, 59 and 61 us; 32 36, 29 and 32; 16 29, 20, 17 and 18; 1 of 2048 x 2048 one 22, four 8.6, eight 7.0,
+  // sixteen 6.4).
   const int64_t waves = met * tiles;
-  const int ks = waves >= 5000 ? 1 : waves >= 2048 ? 2 : waves >= 1024 ? 4 : waves >= 512 || RF > 2 ? 8 : 16;
+  const int ks = waves >= 3000 ? 1 : waves >= 2000 ? 2 : waves >= 1024 ? 4 : waves >= 512 || RF > 2 ? 8 : 16;
   const int per_group = ks > 4 ? 1 : 4 / ks;
   const int cols = (tiles + per_group - 1) / per_group;
   const int64_t blocks = tile_bound(a.rows, a.groups, RF * 16, cols);
@@ -897,7 +909,8 @@ hipError_t thin_typed(const GroupedArgs& a, hipStream_t st) {
 // Offsets in bytes of 16-bit values, a step of 64 rows beyond the last included, fit 32 bits.
 bool short_offsets(int64_t rows, int64_t ld) { return rows > 0 && (rows + 3 * kStep) * ld * 2 < (int64_t)0xf0000000; }
 
-// Tiles of a general kernel: 128 x 128 where there are enough of them, else 64 x 64.
+// Columns of the tiles for any strides: 128 where there are enough of them, else 64 (16 bits, 8,192 rows, 4 groups of 1,001 x 777: 33 us
+// with 128, 46 with 64; 4,096 rows, 4 groups of 500 x 501: 17 and 12).
 bool large_tiles(int64_t row_tiles_128, int64_t cols) { return row_tiles_128 * ((cols + 127) / 128) >= 512; }
 
 template <typename T, int FORM, int TILE>
@@ -923,9 +936,9 @@ hipError_t product_typed(const GroupedArgs& a, bool transpose, hipStream_t st) {
                      short_offsets(a.N, a.ldw);
   if (!transpose) {
     // Up to 8 rows a group the matrices are what takes time, and the kernel for few rows reads them as fast as any (64 groups of
-    // 1024 x 2048 in 16 bits, 64 rows 53 us, tiles 57; 512 rows 73 and 72; in 32 bits 72, tiles of 64 x 64 91).  Beyond, tiles read
-    // them less often (1,024 rows 89 and 72), but where there are few of them a good part of the chip has nothing to do (256 rows,
-    // 4 groups of 2048 x 2048 32 us, tiles 49).
+    // 1024 x 2048 in 16 bits, 64 rows 55 us, tiles 58; 512 rows 59 and 58).  Beyond, tiles read them less often (1,024 rows 64 and
+    // 58), but where there are few of them a good part of the chip has nothing to do (4 groups of 2048 x 2048, 256 rows 27 us, tiles
+    // 31; 8 rows 10 and 30).
     const int side = tiled ? 256 : 64;
     const int64_t row_tiles = a.rows / side + a.groups, tiles = (row_tiles < a.rows ? row_tiles : a.rows) * ((a.N + side - 1) / side);
     if (a.rows <= (int64_t)8 * a.groups) return thin_typed<T, 1>(a, st);

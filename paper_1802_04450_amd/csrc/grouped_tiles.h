@@ -87,7 +87,8 @@ __device__ __forceinline__ RowTile find_tile(const int32_t* offsets, int groups,
 // The same for workgroups that take one tile after the other.  Each die (eight of them, workgroups go to them in turn) has a
 // contiguous eighth of all tiles, column tiles of a row tile side by side, and its workgroups take them side by side: what they read
 // at one time is shared in the die's L2.  Tiles 0 ... count - 1 are this workgroup's.  Where the tiles that would make a last
-// round are for at most half of the workgroups, they are cut in two along the rows, and half() is this workgroup's piece.
+// round are for at most half of the workgroups, they are cut in two along the rows, and half() is this workgroup's piece (5,000 rows,
+// 8 groups of 1024 x 1024 in 16 bits 30 -> 21 us, in 8 bits 28 -> 16).
 // (A group's last tile, which has fewer rows, takes as long as a full one.  All of them at the end, or their missing rows left out
 // of the products, was slower: 615 and 605 instead of 590 us for 65,536 rows in 64 uneven groups, 2048 x 2048.)
 template <int BM>
