@@ -379,7 +379,7 @@ __global__ __launch_bounds__(256, 2) void e4m3_wide_kernel(E4m3Args a, int cols)
 // As in 16 bits: every matrix that is met goes once from memory into the registers of the wave that needs it.  A wave has 16
 // columns and RF * 16 rows; KS of a workgroup's waves (four, or KS if that is more) share the columns, each with every KS-th run of
 // two blocks of the contraction, and their sums are added in order.  Results of 32 bits take the numbers as bf16 (see above).  64 rows,
-// 64 groups of 2048 x 2048 (268 MB) 50 us, 5.3 TB/s.
+// 64 groups of 2048 x 2048 (268 MB) 58 us, 4.6 TB/s.
 constexpr int kThinRun = 2;
 
 template <typename T, int RF, int KS>
@@ -832,10 +832,14 @@ template <typename T, int RF>
 hipError_t thin_typed(const E4m3Args& a, hipStream_t st) {
   const int tiles = (a.N + 15) / 16;
   const int64_t met = a.rows < a.groups ? a.rows : a.groups;  // groups with rows, at most
-  // Waves enough to fill the chip, and no more (64 rows, 64 groups of 2048 x 2048, one, two, four and eight waves for their columns: 50,
-  // 52, 60 and 81 us; 16 rows, 16 groups of 1024 x 2048: 9.5, 9.5, 9.5 and 11).
+  // Where there are many columns, waves with four runs each: more of them have more loads on their way, with fewer runs what a wave
+  // costs shows.  Where there are few, as many as fill the chip.  Measured with the matrices out of memory, rows = groups, one, two,
+  // four and eight waves for the same columns: 32 of 2048 x 4096 67, 66, 64 and 73 us; 64 of 2048 x 2048 57, 58, 64 and 85; of
+  // 2048 x 1024 30, 34, 40 and 65; 4 of 2048 x 4096 20, 14, 12 and 12.
   const int64_t waves = met * tiles;
-  const int ks = waves >= 3000 ? 1 : waves >= 2000 ? 2 : waves >= 1024 ? 4 : waves >= 512 || RF > 2 ? 8 : 16;
+  const int runs = (a.Kp / kScaleBlock + kThinRun - 1) / kThinRun;
+  const int want = waves >= 2000 ? runs / 4 : waves >= 1000 ? 4 : waves >= 500 ? 8 : 16, most = want < runs ? want : runs;
+  const int ks = most >= 16 && waves < 500 && RF <= 2 ? 16 : most >= 8 && waves < 1000 ? 8 : most >= 4 ? 4 : most >= 2 ? 2 : 1;
   const int per_group = ks > 4 ? 1 : 4 / ks;
   const int cols = (tiles + per_group - 1) / per_group;
   const int64_t blocks = tile_bound(a.rows, a.groups, RF * 16, cols);
@@ -862,7 +866,7 @@ hipError_t product_typed(const E4m3Args& a, hipStream_t st) {
   const bool tiled = sizeof(T) == 2 && a.Kp >= 2 * kScaleBlock && a.xrows * a.ldx < (int64_t)1 << 32 && a.N * a.ldw < (int64_t)1 << 32 &&
                      a.xrows * a.ldxs < (int64_t)1 << 32 && a.N * a.ldws < (int64_t)1 << 32;
   // Up to 2 rows a group the matrices are what takes time, and the kernel for few rows reads them as fast as any (64 groups of
-  // 1024 x 2048, 64 rows 27 us, tiles 30).  Beyond, tiles read them less often (256 rows 31 and 29, 1,024 rows 41 and 29), but where
+  // 1024 x 2048 out of memory, 64 rows 32 us, tiles 33).  Beyond, tiles read them less often (256 rows 35 and 34), but where
   // there are few of them a good part of the chip has nothing to do (4 groups of 2048 x 2048, 8 rows 7 us, tiles 19; 256 rows 20
   // and 19).
   const int side = tiled ? 256 : kTile;

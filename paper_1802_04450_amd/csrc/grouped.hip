@@ -352,7 +352,7 @@ __global__ __launch_bounds__(256) void gradient_sum_kernel(Parts parts, const in
 // bounds it.  A wave has 16 columns and RF * 16 rows; KS of a workgroup's four waves share the columns, each with every KS-th
 // run of RUN chunks of the contraction, and their sums are added in order at the end: as few columns as there are, enough
 // waves are at work.  A run of the matrix is on its way while one is used.  Rows of any alignment: a lane's 16 bytes may begin anywhere.
-// 64 rows, 64 groups of 1024 x 2048 in 16 bits (268 MB) 53 us, 5.0 TB/s; 1 row of 2048 x 2048 6.4 us.
+// 64 rows, 64 groups of 2048 x 2048 in 16 bits (537 MB) 126 us, 4.3 TB/s; 1 row of 2048 x 2048 6.4 us.
 constexpr int kThinRun = 4;
 
 template <typename T, int RF, int KS>
@@ -884,11 +884,14 @@ template <typename T, int RF>
 hipError_t thin_typed(const GroupedArgs& a, hipStream_t st) {
   const int tiles = (a.N + 15) / 16;
   const int64_t met = a.rows < a.groups ? a.rows : a.groups;  // groups with rows, at most
-  // Waves enough to fill the chip, and no more (rows = groups, of 1024 x 2048 in 16 bits, one, two, four and eight waves for their
-  // columns: 64 53, 58, 59 and 61 us; 32 36, 29 and 32; 16 29, 20, 17 and 18; 1 of 2048 x 2048 one 22, four 8.6, eight 7.0,
-  // sixteen 6.4).
+  // Where there are many columns, waves with two runs each: more of them have more loads on their way, with fewer runs what a wave costs
+  // shows.  Where there are few, as many as fill the chip.  Measured with the matrices out of memory, 16 bits, rows = groups, one,
+  // two, four and eight waves for the same columns: 64 of 2048 x 2048 164, 142, 133 and 126 us; of 2048 x 1024 74, 71, 73 and 75; of
+  // 2048 x 512 39, 40, 43 and 62; 16 of 1024 x 2048 37, 25, 23 and 24; 1 of 2048 x 2048 34, 19, 11 and 8.
   const int64_t waves = met * tiles;
-  const int ks = waves >= 3000 ? 1 : waves >= 2000 ? 2 : waves >= 1024 ? 4 : waves >= 512 || RF > 2 ? 8 : 16;
+  const int runs = (a.K + kThinRun * 4 * Matrix<T>::kChunk - 1) / (kThinRun * 4 * Matrix<T>::kChunk);
+  const int want = waves >= 2000 ? runs / 2 : waves >= 1000 ? 4 : waves >= 500 ? 8 : 16, most = want < runs ? want : runs;
+  const int ks = most >= 16 && waves < 500 && RF <= 2 ? 16 : most >= 8 ? 8 : most >= 4 ? 4 : most >= 2 ? 2 : 1;
   const int per_group = ks > 4 ? 1 : 4 / ks;
   const int cols = (tiles + per_group - 1) / per_group;
   const int64_t blocks = tile_bound(a.rows, a.groups, RF * 16, cols);
@@ -935,13 +938,13 @@ hipError_t product_typed(const GroupedArgs& a, bool transpose, hipStream_t st) {
                      a.K % CH == 0 && a.N % CH == 0 && whole_chunks<T>(a.y, a.ldy) && short_offsets(a.xrows, a.ldx) &&
                      short_offsets(a.N, a.ldw);
   if (!transpose) {
-    // Up to 8 rows a group the matrices are what takes time, and the kernel for few rows reads them as fast as any (64 groups of
-    // 1024 x 2048 in 16 bits, 64 rows 55 us, tiles 58; 512 rows 59 and 58).  Beyond, tiles read them less often (1,024 rows 64 and
-    // 58), but where there are few of them a good part of the chip has nothing to do (4 groups of 2048 x 2048, 256 rows 27 us, tiles
-    // 31; 8 rows 10 and 30).
+    // Up to 4 rows a group the matrices are what takes time, and the kernel for few rows reads them as fast as any (64 groups of
+    // 1024 x 2048 in 16 bits out of memory, 64 rows 73 us, tiles 74; 64 rows in groups of 0 to 8 46 and 55).  Beyond, tiles read them
+    // less often (512 rows 79 and 74), but where there are few of them a good part of the chip has nothing to do (4 groups of 2048 x
+    // 2048, 256 rows 27 us, tiles 31; 8 rows 10 and 30).
     const int side = tiled ? 256 : 64;
     const int64_t row_tiles = a.rows / side + a.groups, tiles = (row_tiles < a.rows ? row_tiles : a.rows) * ((a.N + side - 1) / side);
-    if (a.rows <= (int64_t)8 * a.groups) return thin_typed<T, 1>(a, st);
+    if (a.rows <= (int64_t)4 * a.groups) return thin_typed<T, 1>(a, st);
     if (tiles < (tiled ? 128 : 512) && a.rows <= (int64_t)64 * a.groups)
       return a.rows <= (int64_t)24 * a.groups ? thin_typed<T, 2>(a, st) : thin_typed<T, 4>(a, st);
   }
