@@ -223,7 +223,7 @@ __device__ __forceinline__ int32_t take_place(int32_t c, int bits, int lane, int
 }
 __device__ __forceinline__ int bits_of(int k) { return k > 1 ? 32 - __builtin_clz(k - 1) : 0; }
 
-// Few slots: assignment and grouping in one workgroup (8 rows of 64, t = 4: 3.3 us, about what an empty launch takes).
+// Few slots: assignment and grouping in one workgroup (8 rows of 64, t = 4: 3.5 us, about what an empty launch takes).
 constexpr int kSmallThreads = 1024, kSmallSlots = 512, kSmallClusters = 512;
 template <typename T, int LANES, int VPL, bool WIDE>
 __global__ __launch_bounds__(kSmallThreads) void route_small_kernel(const T* __restrict__ scores, int64_t ld,
@@ -581,7 +581,7 @@ __device__ __forceinline__ void store_part(T* p, const float (&v)[E]) {
 }
 
 // out_i = sum_s w_is z_place(i,s), added in the order of s, one thread an E of them.  The grouped rows that it gathers are what it takes
-// (16 rows, 4 slots, 2,048 values: 3.6 us, about what an empty launch takes).
+// (16 rows, 4 slots, 2,048 values: 3.3 us, about what an empty launch takes).
 template <typename T, int E>
 __global__ __launch_bounds__(kThreads) void combine_kernel(const T* __restrict__ z, int64_t ldz, int64_t rows,
                                                            const int32_t* __restrict__ place, const float* __restrict__ weight,
