@@ -247,12 +247,14 @@ __global__ __launch_bounds__(256) void grouped_any_kernel(const T* __restrict__ 
 #pragma unroll
     for (int u = 0; u < LR; ++u) {
       if (__any(rs[u])) r[u] = shifted<T>(r[u], rs[u]);
-      *reinterpret_cast<Chunk*>(R_ALONG ? rt + along_row(u) * ALONG + along_e(u) : rt + across_e(u, TR) * RACROSS + across_col(u, TR)) = r[u];
+      T* at = R_ALONG ? rt + along_row(u) * ALONG + along_e(u) : rt + across_e(u, TR) * RACROSS + across_col(u, TR);
+      *reinterpret_cast<Chunk*>(at) = r[u];
     }
 #pragma unroll
     for (int u = 0; u < LC; ++u) {
       if (__any(cs[u])) c[u] = shifted<T>(c[u], cs[u]);
-      *reinterpret_cast<Chunk*>(C_ALONG ? ct + along_row(u) * ALONG + along_e(u) : ct + across_e(u, TC) * CACROSS + across_col(u, TC)) = c[u];
+      T* at = C_ALONG ? ct + along_row(u) * ALONG + along_e(u) : ct + across_e(u, TC) * CACROSS + across_col(u, TC);
+      *reinterpret_cast<Chunk*>(at) = c[u];
     }
   };
   // Rows (columns) first ... first + 15 of an operand, the kk-th 4 chunks of the step.
@@ -442,9 +444,9 @@ __global__ __launch_bounds__(KS > 4 ? KS * 64 : 256) void grouped_thin_kernel(Gr
 // tile's results are stored while the next one's products run.  For that every tile has at least two steps, a gradient's three, as
 // the rows of x that a step takes are looked up a step before they are fetched; steps behind the contraction's end hold zeros.
 //
-// 65,536 rows, 64 groups of 2048 x 2048 in 16 bits: product and transposed 465 us (1,180 TFLOP/s), gradient 612 (900, its operands
+// 65,536 rows, 64 groups of 2048 x 2048 in 16 bits: product and transposed 472 us (1,165 TFLOP/s), gradient 580 (950, its operands
 // both turned on the way out of LDS).  What bounds it is the matrix instructions' rate at the power they take: on operands of zeros
-// the same product takes a quarter less.  Four waves with 128 x 128 each read LDS less often, but spill or move registers to
+// the same product takes 387.  The rows in any other order: 471 to 479; to copy them into that order first would take 97.  Four waves with 128 x 128 each read LDS less often, but spill or move registers to
 // and fro; 32 x 32 instructions, wave priorities and all tiles of 128 rows were no faster.
 constexpr int kStep = 64;
 constexpr uint32_t kNowhere = 0xfffffff0u;  // an offset behind every buffer's end: reads as zeros
