@@ -446,8 +446,9 @@ __global__ __launch_bounds__(KS > 4 ? KS * 64 : 256) void grouped_thin_kernel(Gr
 //
 // 65,536 rows, 64 groups of 2048 x 2048 in 16 bits: product and transposed 472 us (1,165 TFLOP/s), gradient 580 (950, its operands
 // both turned on the way out of LDS).  What bounds it is the matrix instructions' rate at the power they take: on operands of zeros
-// the same product takes 387.  The rows in any other order: 471 to 479; to copy them into that order first would take 97.  Four waves with 128 x 128 each read LDS less often, but spill or move registers to
-// and fro; 32 x 32 instructions, wave priorities and all tiles of 128 rows were no faster.
+// the same product takes 387.  The rows in any other order: 471 to 479; to copy them into that order first would take 97.  Four
+// waves with 128 x 128 each read LDS less often, but spill or move registers to and fro; 32 x 32 instructions and wave priorities
+// were no faster.
 constexpr int kStep = 64;
 constexpr uint32_t kNowhere = 0xfffffff0u;  // an offset behind every buffer's end: reads as zeros
 
